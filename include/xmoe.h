@@ -67,7 +67,9 @@ typedef enum {
     XMOE_WS_BUILD_ERI_CAPPED = 4, /* rows = T          */
     XMOE_WS_MLP2_FWD = 5,       /* rows = B            */
     XMOE_WS_MLP2_BWD = 6,       /* rows = B            */
-    XMOE_WS_RBD_STAGE0 = 7      /* rows = T            */
+    XMOE_WS_RBD_STAGE0 = 7,     /* rows = T            */
+    /* 8 to 15 name no call */
+    XMOE_WS_ADD_RMSNORM_BWD = 16 /* rows = T           */
 } xmoe_ws_op;
 
 /* activation of the two-matrix expert (xmoe_expert_mlp2_fwd / _bwd) */
@@ -79,6 +81,9 @@ typedef enum {
 
 /* Largest expert count the routing / ERI kernels accept. */
 #define XMOE_MAX_EXPERTS 512
+
+/* Largest width of the norm. */
+#define XMOE_MAX_NORM_WIDTH 16384
 
 /* Human-readable name of a status code (static storage). */
 const char* xmoe_status_string(int status);
@@ -336,6 +341,36 @@ int xmoe_route_bwd_rows(const float* logits, const int32_t* topk_idx, const floa
  */
 int xmoe_gate_logits_bwd(const void* x, const void* w_router, const float* dlogits, int T, int d, int E, int dt,
                          void* dw_router, void* dx_gate, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * The root-mean-square norm in front of the layer, with the residual's addition:
+ *   h[t,:] = x[t,:] + residual[t,:], rounded to dt;   r[t] = 1 / sqrt(mean_i h[t,i]^2 + eps);
+ *   y[t,i] = h[t,i] * r[t] * gain[i]
+ * x [T,d], residual [T,d] or NULL (h is x then), gain [d], all dt; eps > 0.  Outputs: h [T,d] dt, may be x or residual,
+ * required with a residual and else optional (NULL); at least one of y [T,d] dt and q; rstd [T] float32 or NULL: r, for the
+ * backward.
+ * 8-bit rows, q and q_scale (both or neither):  q[t,i] = rint(h[t,i] * gain[i] * (127 / m)) with m = max_i |h[t,i] * gain[i]|,
+ * q_scale[t] = m * r[t] / 127, so that q_scale * q is y up to half a q_scale.  q is int8 in rows of xmoe_q8_pitch(d) bytes,
+ * zeros behind the first d, 16-byte aligned; q_scale [T] float32.  A row with m below 2^-120 counts as zero (q = 0,
+ * q_scale = 0).  The integers do not depend on the order of any sum.
+ * The mean of the squares is a float32 sum: it has to stay finite.  A row that holds an infinity or a NaN gives NaN in
+ * the affected y, and a q_scale that is not finite.
+ * d <= XMOE_MAX_NORM_WIDTH.
+ */
+int xmoe_add_rmsnorm(const void* x, const void* residual, const void* gain, int T, int d, float eps, int dt, void* h,
+                     void* y, void* q, float* q_scale, float* rstd, void* stream);
+
+/* Backward of the norm.  With n = h * rstd and v = dy * gain:
+ *   dx[t,i] = rstd[t] * (v[t,i] - n[t,i] * mean_j(v[t,j] * n[t,j])) + dh[t,i];      dgain[i] = sum_t dy[t,i] * n[t,i]
+ * dy [T,d]: gradient of y; dh [T,d] or NULL: gradient that reaches h by other ways (the residual stream); h, rstd: of the
+ * forward call (x itself where h was not asked for).  dx [T,d] dt (out): gradient of x, and of residual; dgain [d] dt (out),
+ * overwritten (zero for T = 0).  The outputs overlap no input.  ws: XMOE_WS_ADD_RMSNORM_BWD bytes.
+ */
+int xmoe_add_rmsnorm_bwd(const void* dy, const void* dh, const void* h, const void* gain, const float* rstd, int T, int d,
+                         int dt, void* dx, void* dgain, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of an 8-bit row of n values: n rounded up to a multiple of 128.  Host-only, pure. */
+int xmoe_q8_pitch(int n);
 
 /* ---------------------------------------------------------------------------------------------------------
  * Optional per-kernel timing with HIP events on the caller's stream (for benchmarks).  Off by default.

@@ -16,6 +16,7 @@ from ._lib import lib
 XMOE_F32, XMOE_BF16 = 0, 1
 WS_BUILD_ERI, WS_FFN_FWD, WS_FFN_BWD, WS_GATE_BWD, WS_BUILD_ERI_CAPPED, WS_MLP2_FWD, WS_MLP2_BWD = 0, 1, 2, 3, 4, 5, 6
 WS_RBD_STAGE0 = 7
+WS_ADD_RMSNORM_BWD = 16
 ACT_CODES = {"identity": 0, "gelu": 1, "silu": 2}   # xmoe_act
 
 __all__ = [
@@ -26,6 +27,7 @@ __all__ = [
     "XMOE_F32", "XMOE_BF16", "WS_BUILD_ERI", "WS_FFN_FWD", "WS_FFN_BWD", "WS_GATE_BWD", "WS_BUILD_ERI_CAPPED", "xmoe_build_eri_capped",
     "xmoe_expert_mlp2_fwd", "xmoe_expert_mlp2_bwd", "WS_MLP2_FWD", "WS_MLP2_BWD", "ACT_CODES",
     "xmoe_rbd_stage0", "xmoe_rbd_absolute_index", "WS_RBD_STAGE0", "xmoe_build_eri_static", "xmoe_combine_bwd_weights", "xmoe_append_shared_segments",
+    "xmoe_add_rmsnorm", "xmoe_add_rmsnorm_bwd", "WS_ADD_RMSNORM_BWD", "xmoe_q8_pitch",
 ]
 
 
@@ -370,6 +372,38 @@ def xmoe_gate_logits_bwd(x, w_router, dlogits, dw_router, dx_gate, ws) -> None:
                                       _ptr(dlogits, torch.float32, "dlogits"), T, d, E, dtype_code(dt),
                                       _ptr(dw_router, dt, "dw_router"), _ptr(dx_gate, dt, "dx_gate"),
                                       _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()), "xmoe_gate_logits_bwd")
+
+
+def xmoe_q8_pitch(n: int) -> int:
+    """Bytes of an 8-bit row of n values."""
+    return lib().xmoe_q8_pitch(n)
+
+
+def xmoe_add_rmsnorm(x, residual, gain, eps: float, h, y=None, q=None, q_scale=None, rstd=None) -> None:
+    """h = x + residual; y = h / rms(h) * gain, and / or the same as 8-bit rows q [T, xmoe_q8_pitch(d)] int8 with q_scale [T].
+    h may be x or residual; None only without a residual (which may be None: h is x then)."""
+    T, d = x.shape
+    dt = x.dtype
+    assert gain.numel() == d and (residual is None or residual.shape == x.shape)
+    assert (h is None or h.shape == x.shape) and (y is None or y.shape == x.shape)
+    assert q is None or (q.shape[0] == T and q.shape[1] == xmoe_q8_pitch(d) and q.dim() == 2)
+    assert (q_scale is None or q_scale.numel() == T) and (rstd is None or rstd.numel() == T)
+    _check(lib().xmoe_add_rmsnorm(_ptr(x, None, "x"), _ptr(residual, dt, "residual"), _ptr(gain, dt, "gain"), T, d,
+                                  float(eps), dtype_code(dt), _ptr(h, dt, "h"), _ptr(y, dt, "y"), _ptr(q, torch.int8, "q"),
+                                  _ptr(q_scale, torch.float32, "q_scale"), _ptr(rstd, torch.float32, "rstd"), _stream()),
+           "xmoe_add_rmsnorm")
+
+
+def xmoe_add_rmsnorm_bwd(dy, dh, h, gain, rstd, dx, dgain, ws) -> None:
+    """dh: None, or the gradient that reaches h by other ways."""
+    T, d = h.shape
+    dt = h.dtype
+    assert tuple(dy.shape) == (T, d) and tuple(dx.shape) == (T, d) and (dh is None or tuple(dh.shape) == (T, d))
+    assert gain.numel() == d and dgain.numel() == d and rstd.numel() == T
+    _check(lib().xmoe_add_rmsnorm_bwd(_ptr(dy, dt, "dy"), _ptr(dh, dt, "dh"), _ptr(h, None, "h"), _ptr(gain, dt, "gain"),
+                                      _ptr(rstd, torch.float32, "rstd"), T, d, dtype_code(dt), _ptr(dx, dt, "dx"),
+                                      _ptr(dgain, dt, "dgain"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
+           "xmoe_add_rmsnorm_bwd")
 
 
 def xmoe_prof_enable(on: bool) -> None:

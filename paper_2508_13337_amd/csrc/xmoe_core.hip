@@ -72,6 +72,9 @@ const char* const kKernelNames[K_COUNT] = {
     "mlp2_dact_direct_kernel",
     "ffn_wgrad_direct_kernel",
     "ffn_bwd_wgrads_dma_kernel",
+    "add_rmsnorm_kernel",
+    "add_rmsnorm_bwd_kernel",
+    "norm_dgain_kernel",
 };
 
 hipEvent_t get_event() {
@@ -154,9 +157,12 @@ size_t xmoe_workspace_bytes(int op, int rows, int d, int E, int k, int f, int dt
         case XMOE_WS_MLP2_FWD: return mlp2_fwd_ws_bytes(rows, E, d, f, dt);
         case XMOE_WS_MLP2_BWD: return mlp2_bwd_ws_bytes(rows, E, d, f, dt);
         case XMOE_WS_RBD_STAGE0: return rbd_ws_bytes(rows, k);
+        case XMOE_WS_ADD_RMSNORM_BWD: return norm_bwd_ws_bytes(rows, d);
         default: return 0;
     }
 }
+
+int xmoe_q8_pitch(int n) { return q8_pitch(n); }
 
 void xmoe_prof_enable(int on) { g_prof.on = (on != 0); }
 

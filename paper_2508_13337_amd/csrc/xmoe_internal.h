@@ -64,6 +64,9 @@ enum KernelId : int {
     K_MLP2_DACT_DIRECT,
     K_FFN_WGRAD_DIRECT,
     K_FFN_BWD_WGRADS_DMA,   // ffn_bwd_rest_dma_kernel without dX
+    K_ADD_RMSNORM,
+    K_ADD_RMSNORM_BWD,
+    K_NORM_DGAIN,
     K_COUNT
 };
 

@@ -82,4 +82,14 @@ static inline size_t gate_bwd_ws_bytes(int T, int d, int E) {
     return align_up((size_t)gate_bwd_splits(T) * (size_t)d * (size_t)E * sizeof(float), 256);
 }
 
+// ----- 8-bit rows: bytes of a row of n values -----
+static inline int q8_pitch(int n) { return (n + 127) / 128 * 128; }
+
+// ----- norm backward: one partial row of dgain per block (two blocks per CU) -----
+static inline int norm_bwd_blocks(int T) { return T < 512 ? T : 512; }
+static inline size_t norm_bwd_ws_bytes(int T, int d) {
+    const int blocks = norm_bwd_blocks(T);
+    return align_up((size_t)(blocks > 0 ? blocks : 1) * (size_t)d * sizeof(float), 256);
+}
+
 }  // namespace xmoe
