@@ -69,7 +69,8 @@ typedef enum {
     XMOE_WS_MLP2_BWD = 6,       /* rows = B            */
     XMOE_WS_RBD_STAGE0 = 7,     /* rows = T            */
     /* 8 to 15 name no call */
-    XMOE_WS_ADD_RMSNORM_BWD = 16 /* rows = T           */
+    XMOE_WS_ADD_RMSNORM_BWD = 16, /* rows = T          */
+    XMOE_WS_FFN_Q8_FWD = 17     /* rows = B            */
 } xmoe_ws_op;
 
 /* activation of the two-matrix expert (xmoe_expert_mlp2_fwd / _bwd) */
@@ -84,6 +85,8 @@ typedef enum {
 
 /* Largest width of the norm. */
 #define XMOE_MAX_NORM_WIDTH 16384
+/* Largest width of an 8-bit row in a product (the sums are int32). */
+#define XMOE_MAX_Q8_WIDTH 65536
 
 /* Human-readable name of a status code (static storage). */
 const char* xmoe_status_string(int status);
@@ -355,7 +358,7 @@ int xmoe_gate_logits_bwd(const void* x, const void* w_router, const float* dlogi
  * q_scale = 0).  The integers do not depend on the order of any sum.
  * The mean of the squares is a float32 sum: it has to stay finite.  A row that holds an infinity or a NaN gives NaN in
  * the affected y, and a q_scale that is not finite.
- * d <= XMOE_MAX_NORM_WIDTH.
+ * d <= XMOE_MAX_NORM_WIDTH, T < 2^22.
  */
 int xmoe_add_rmsnorm(const void* x, const void* residual, const void* gain, int T, int d, float eps, int dt, void* h,
                      void* y, void* q, float* q_scale, float* rstd, void* stream);
@@ -371,6 +374,30 @@ int xmoe_add_rmsnorm_bwd(const void* dy, const void* dh, const void* h, const vo
 
 /* Bytes of an 8-bit row of n values: n rounded up to a multiple of 128.  Host-only, pure. */
 int xmoe_q8_pitch(int n);
+
+/* Weights as 8-bit integers with one scale for each output column, for xmoe_expert_ffn_q8_fwd: for each expert e and
+ * column n, m = max_k |w[e,k,n]|,  wq[e,n,k] = rint(w[e,k,n] * (127 / m)),  scale[e,n] = m / 127   (0 where m < 2^-120).
+ * w [E,K,N] dt ("in x out"); wq [E,N,xmoe_q8_pitch(K)] int8 (out), K-contiguous, zeros behind the first K of a row, 16-byte
+ * aligned; scale [E,N] float32 (out).  Done once for a model's weights.  K <= XMOE_MAX_Q8_WIDTH, E <= 65535.
+ */
+int xmoe_quantize_weights(const void* w, int E, int K, int N, int dt, void* wq, float* scale, void* stream);
+
+/* The SwiGLU experts (xmoe_expert_ffn_fwd) on 8-bit integers, forward only (serving): for each expert e and its rows r,
+ *   G[r,n] = x_scale[r] g_scale[e,n] sum_k xq[r,k] wgq[e,n,k],  U likewise with wuq, u_scale;   A = silu(G) * U;
+ *   aq[r,:], as[r] = A's row as 8-bit integers with one scale, as xmoe_add_rmsnorm makes them;
+ *   Y[r,n] = as[r] d_scale[e,n] sum_k aq[r,k] wdq[e,n,k]
+ * The sums over k are exact integers.  On its way to aq, A is held as 16-bit integers relative to the largest of 32 columns.
+ * xq: int8 rows of xmoe_q8_pitch(d) bytes (xmoe_add_rmsnorm's q), x_scale float32, one for each; row_index, expert_offsets,
+ * B, E as in xmoe_expert_ffn_fwd (with row_index, xq and x_scale are the tokens' and row i is row row_index[i] of both).
+ * wgq, wuq [E,f,xmoe_q8_pitch(d)], wdq [E,d,xmoe_q8_pitch(f)] int8; g_scale, u_scale [E,f], d_scale [E,d] float32
+ * (xmoe_quantize_weights); 8-bit operands 16-byte aligned, with zeros behind the values of each row.  y [B,d] dt (out); rows
+ * of y outside every segment are not written.  A scale that is not finite makes the rows it reaches not finite.
+ * A row's result does not depend on the call's other rows.  d, f <= XMOE_MAX_Q8_WIDTH, B < 2^26.  ws: XMOE_WS_FFN_Q8_FWD bytes.
+ */
+int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* row_index, const int32_t* expert_offsets,
+                           int B, int E, int d, int f, const void* wgq, const float* g_scale, const void* wuq,
+                           const float* u_scale, const void* wdq, const float* d_scale, void* y, int dt, void* ws,
+                           size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------------
  * Optional per-kernel timing with HIP events on the caller's stream (for benchmarks).  Off by default.

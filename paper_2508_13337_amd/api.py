@@ -16,7 +16,7 @@ from ._lib import lib
 XMOE_F32, XMOE_BF16 = 0, 1
 WS_BUILD_ERI, WS_FFN_FWD, WS_FFN_BWD, WS_GATE_BWD, WS_BUILD_ERI_CAPPED, WS_MLP2_FWD, WS_MLP2_BWD = 0, 1, 2, 3, 4, 5, 6
 WS_RBD_STAGE0 = 7
-WS_ADD_RMSNORM_BWD = 16
+WS_ADD_RMSNORM_BWD, WS_FFN_Q8_FWD = 16, 17
 ACT_CODES = {"identity": 0, "gelu": 1, "silu": 2}   # xmoe_act
 
 __all__ = [
@@ -28,6 +28,7 @@ __all__ = [
     "xmoe_expert_mlp2_fwd", "xmoe_expert_mlp2_bwd", "WS_MLP2_FWD", "WS_MLP2_BWD", "ACT_CODES",
     "xmoe_rbd_stage0", "xmoe_rbd_absolute_index", "WS_RBD_STAGE0", "xmoe_build_eri_static", "xmoe_combine_bwd_weights", "xmoe_append_shared_segments",
     "xmoe_add_rmsnorm", "xmoe_add_rmsnorm_bwd", "WS_ADD_RMSNORM_BWD", "xmoe_q8_pitch",
+    "xmoe_quantize_weights", "xmoe_expert_ffn_q8_fwd", "WS_FFN_Q8_FWD",
 ]
 
 
@@ -404,6 +405,34 @@ def xmoe_add_rmsnorm_bwd(dy, dh, h, gain, rstd, dx, dgain, ws) -> None:
                                       _ptr(rstd, torch.float32, "rstd"), T, d, dtype_code(dt), _ptr(dx, dt, "dx"),
                                       _ptr(dgain, dt, "dgain"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
            "xmoe_add_rmsnorm_bwd")
+
+
+def xmoe_quantize_weights(w, wq, scale) -> None:
+    """w [E, K, N] -> wq [E, N, xmoe_q8_pitch(K)] int8 and scale [E, N]: what xmoe_expert_ffn_q8_fwd takes."""
+    E, K, N = w.shape
+    assert tuple(wq.shape) == (E, N, xmoe_q8_pitch(K)) and tuple(scale.shape) == (E, N)
+    _check(lib().xmoe_quantize_weights(_ptr(w, None, "w"), E, K, N, dtype_code(w.dtype), _ptr(wq, torch.int8, "wq"),
+                                       _ptr(scale, torch.float32, "scale"), _stream()), "xmoe_quantize_weights")
+
+
+def xmoe_expert_ffn_q8_fwd(xq, x_scale, expert_offsets, wgq, g_scale, wuq, u_scale, wdq, d_scale, y, ws,
+                           row_index=None) -> None:
+    """The SwiGLU experts on 8-bit rows xq (with x_scale) and 8-bit weights; y [B, d] in float32 or bfloat16.  row_index:
+    as in xmoe_expert_ffn_fwd."""
+    B, d = y.shape
+    E, f = g_scale.shape
+    dp, fp = xmoe_q8_pitch(d), xmoe_q8_pitch(f)
+    assert xq.dim() == 2 and xq.shape[1] == dp and x_scale.numel() == xq.shape[0]
+    assert (xq.shape[0] if row_index is None else row_index.numel()) == B and expert_offsets.numel() == E + 1
+    assert tuple(wgq.shape) == (E, f, dp) and wuq.shape == wgq.shape and u_scale.shape == g_scale.shape
+    assert tuple(wdq.shape) == (E, d, fp) and tuple(d_scale.shape) == (E, d)
+    i8, f32, i32 = torch.int8, torch.float32, torch.int32
+    _check(lib().xmoe_expert_ffn_q8_fwd(
+        _ptr(xq, i8, "xq"), _ptr(x_scale, f32, "x_scale"), _ptr(row_index, i32, "row_index"),
+        _ptr(expert_offsets, i32, "expert_offsets"), B, E, d, f, _ptr(wgq, i8, "wgq"), _ptr(g_scale, f32, "g_scale"),
+        _ptr(wuq, i8, "wuq"), _ptr(u_scale, f32, "u_scale"), _ptr(wdq, i8, "wdq"), _ptr(d_scale, f32, "d_scale"),
+        _ptr(y, None, "y"), dtype_code(y.dtype), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
+        "xmoe_expert_ffn_q8_fwd")
 
 
 def xmoe_prof_enable(on: bool) -> None:

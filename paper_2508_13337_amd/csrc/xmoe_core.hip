@@ -75,6 +75,10 @@ const char* const kKernelNames[K_COUNT] = {
     "add_rmsnorm_kernel",
     "add_rmsnorm_bwd_kernel",
     "norm_dgain_kernel",
+    "quantize_weights_kernel",
+    "q8_gateup_kernel",
+    "q8_rows_kernel",
+    "q8_down_kernel",
 };
 
 hipEvent_t get_event() {
@@ -158,6 +162,7 @@ size_t xmoe_workspace_bytes(int op, int rows, int d, int E, int k, int f, int dt
         case XMOE_WS_MLP2_BWD: return mlp2_bwd_ws_bytes(rows, E, d, f, dt);
         case XMOE_WS_RBD_STAGE0: return rbd_ws_bytes(rows, k);
         case XMOE_WS_ADD_RMSNORM_BWD: return norm_bwd_ws_bytes(rows, d);
+        case XMOE_WS_FFN_Q8_FWD: return ffn_q8_ws_bytes(rows, E, f);
         default: return 0;
     }
 }

@@ -67,6 +67,10 @@ enum KernelId : int {
     K_ADD_RMSNORM,
     K_ADD_RMSNORM_BWD,
     K_NORM_DGAIN,
+    K_QUANTIZE_WEIGHTS,
+    K_Q8_GATEUP,
+    K_Q8_ROWS,
+    K_Q8_DOWN,
     K_COUNT
 };
 

@@ -363,7 +363,7 @@ int launch_norm_bwd(const void* dy, const void* dh, const void* h, const void* g
 
 int check_norm(int T, int d, int dt) {
     if (!dtype_ok(dt)) return XMOE_ERR_UNSUPPORTED;
-    if (T < 0 || d < 1) return XMOE_ERR_INVALID_ARG;
+    if (T < 0 || d < 1 || T >= (1 << 22)) return XMOE_ERR_INVALID_ARG;   // a grid has fewer than 2^32 threads
     if (d > XMOE_MAX_NORM_WIDTH) return XMOE_ERR_UNSUPPORTED;
     return XMOE_OK;
 }

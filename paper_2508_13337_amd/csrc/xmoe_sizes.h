@@ -85,6 +85,13 @@ static inline size_t gate_bwd_ws_bytes(int T, int d, int E) {
 // ----- 8-bit rows: bytes of a row of n values -----
 static inline int q8_pitch(int n) { return (n + 127) / 128 * 128; }
 
+// ----- experts on 8-bit integers: tile map | A as 16-bit integers, the maxima of every 32 columns | A's 8-bit rows, scales
+static inline size_t ffn_q8_ws_bytes(int B, int E, int f) {
+    const size_t b = B > 0 ? B : 1, fp = q8_pitch(f);
+    return ffn_tilemap_bytes(B, E) + align_up(b * fp * 2, 256) + align_up(b * (fp / 32) * 4, 256) + align_up(b * fp, 256) +
+           align_up(b * 4, 256);
+}
+
 // ----- norm backward: one partial row of dgain per block (two blocks per CU) -----
 static inline int norm_bwd_blocks(int T) { return T < 512 ? T : 512; }
 static inline size_t norm_bwd_ws_bytes(int T, int d) {
