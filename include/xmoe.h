@@ -70,7 +70,8 @@ typedef enum {
     XMOE_WS_RBD_STAGE0 = 7,     /* rows = T            */
     /* 8 to 15 name no call */
     XMOE_WS_ADD_RMSNORM_BWD = 16, /* rows = T          */
-    XMOE_WS_FFN_Q8_FWD = 17     /* rows = B            */
+    XMOE_WS_FFN_Q8_FWD = 17,    /* rows = B            */
+    XMOE_WS_LAYER_FEW_FWD = 18  /* rows = T, k = k + E_s, E = E + E_s */
 } xmoe_ws_op;
 
 /* activation of the two-matrix expert (xmoe_expert_mlp2_fwd / _bwd) */
@@ -87,6 +88,9 @@ typedef enum {
 #define XMOE_MAX_NORM_WIDTH 16384
 /* Largest width of an 8-bit row in a product (the sums are int32). */
 #define XMOE_MAX_Q8_WIDTH 65536
+/* Most tokens, and largest widths, of xmoe_layer_few_fwd. */
+#define XMOE_FEW_TOKENS 32
+#define XMOE_MAX_FEW_WIDTH 65536
 
 /* Human-readable name of a status code (static storage). */
 const char* xmoe_status_string(int status);
@@ -398,6 +402,21 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
                            int B, int E, int d, int f, const void* wgq, const float* g_scale, const void* wuq,
                            const float* u_scale, const void* wdq, const float* d_scale, void* y, int dt, void* ws,
                            size_t ws_bytes, void* stream);
+
+/* A whole layer for a few tokens (a decoding step), forward only: xmoe_gate_logits, xmoe_route, the SwiGLU experts and
+ * xmoe_combine in two or three launches, without index arrays:
+ *   out[t,:] = sum_j topk_w[t,j] * FFN_e(x[t]) with e = topk_idx[t,j], + sum_s FFN_{E+s}(x[t]) (+ addend[t,:])
+ * x [T,d], w_router [d,E], bias [E] float32 or NULL, wg, wu [E+E_s,d,f], wd [E+E_s,f,d] (the shared experts behind the routed
+ * ones), addend [T,d] or NULL, all dt but bias.  Outputs: logits [T,E], topk_idx, topk_w [T,k] as xmoe_gate_logits and
+ * xmoe_route give them, bit for bit; out [T,d] dt, may be addend.  A is stored as dt, the experts' outputs are not rounded
+ * before their sum.  T <= XMOE_FEW_TOKENS, E + E_s <= XMOE_MAX_EXPERTS, k <= 64, d, f <= XMOE_MAX_FEW_WIDTH.  An expert that no
+ * token picked is not read.  A token's row of out does not depend on the call's other tokens.
+ * ws: XMOE_WS_LAYER_FEW_FWD bytes, of one call at a time.
+ */
+int xmoe_layer_few_fwd(const void* x, const void* w_router, const float* bias, const void* wg, const void* wu,
+                       const void* wd, const void* addend, int T, int d, int E, int E_s, int k, int f, int dt,
+                       float* logits, int32_t* topk_idx, float* topk_w, void* out, void* ws, size_t ws_bytes,
+                       void* stream);
 
 /* ---------------------------------------------------------------------------------------------------------
  * Optional per-kernel timing with HIP events on the caller's stream (for benchmarks).  Off by default.

@@ -46,6 +46,7 @@ SIGNATURES = {
     "xmoe_quantize_weights": (_c_int, [_c_void_p] + [_c_int] * 4 + [_c_void_p] * 3),
     "xmoe_expert_ffn_q8_fwd": (_c_int, [_c_void_p] * 4 + [_c_int] * 4 + [_c_void_p] * 7 + [_c_int, _c_void_p, _c_size_t,
                                                                                            _c_void_p]),
+    "xmoe_layer_few_fwd": (_c_int, [_c_void_p] * 7 + [_c_int] * 7 + [_c_void_p] * 5 + [_c_size_t, _c_void_p]),
     "xmoe_q8_pitch": (_c_int, [_c_int]),
     "xmoe_prof_enable": (None, [_c_int]),
     "xmoe_prof_reset": (None, []),

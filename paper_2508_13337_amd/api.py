@@ -16,7 +16,8 @@ from ._lib import lib
 XMOE_F32, XMOE_BF16 = 0, 1
 WS_BUILD_ERI, WS_FFN_FWD, WS_FFN_BWD, WS_GATE_BWD, WS_BUILD_ERI_CAPPED, WS_MLP2_FWD, WS_MLP2_BWD = 0, 1, 2, 3, 4, 5, 6
 WS_RBD_STAGE0 = 7
-WS_ADD_RMSNORM_BWD, WS_FFN_Q8_FWD = 16, 17
+WS_ADD_RMSNORM_BWD, WS_FFN_Q8_FWD, WS_LAYER_FEW_FWD = 16, 17, 18
+FEW_TOKENS = 32   # XMOE_FEW_TOKENS
 ACT_CODES = {"identity": 0, "gelu": 1, "silu": 2}   # xmoe_act
 
 __all__ = [
@@ -29,6 +30,7 @@ __all__ = [
     "xmoe_rbd_stage0", "xmoe_rbd_absolute_index", "WS_RBD_STAGE0", "xmoe_build_eri_static", "xmoe_combine_bwd_weights", "xmoe_append_shared_segments",
     "xmoe_add_rmsnorm", "xmoe_add_rmsnorm_bwd", "WS_ADD_RMSNORM_BWD", "xmoe_q8_pitch",
     "xmoe_quantize_weights", "xmoe_expert_ffn_q8_fwd", "WS_FFN_Q8_FWD",
+    "xmoe_layer_few_fwd", "WS_LAYER_FEW_FWD", "FEW_TOKENS",
 ]
 
 
@@ -433,6 +435,25 @@ def xmoe_expert_ffn_q8_fwd(xq, x_scale, expert_offsets, wgq, g_scale, wuq, u_sca
         _ptr(wuq, i8, "wuq"), _ptr(u_scale, f32, "u_scale"), _ptr(wdq, i8, "wdq"), _ptr(d_scale, f32, "d_scale"),
         _ptr(y, None, "y"), dtype_code(y.dtype), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
         "xmoe_expert_ffn_q8_fwd")
+
+
+def xmoe_layer_few_fwd(x, w_router, bias, wg, wu, wd, addend, logits, topk_idx, topk_w, out, ws) -> None:
+    """A whole layer for at most FEW_TOKENS tokens.  wg, wu, wd: the routed experts' matrices, then the shared experts'.
+    addend: None, or [T, d]; out may be addend.  ws: WS_LAYER_FEW_FWD bytes, sized with k + E_s and E + E_s."""
+    T, d = x.shape
+    E, k = w_router.shape[1], topk_idx.shape[1]
+    Ea, d2, f = wg.shape
+    dt = x.dtype
+    assert w_router.shape[0] == d and d2 == d and Ea >= E and (bias is None or bias.numel() == E)
+    assert wu.shape == wg.shape and tuple(wd.shape) == (Ea, f, d) and (addend is None or addend.shape == x.shape)
+    assert tuple(logits.shape) == (T, E) and topk_idx.shape[0] == T and topk_w.shape == topk_idx.shape
+    assert out.shape == x.shape
+    f32 = torch.float32
+    _check(lib().xmoe_layer_few_fwd(
+        _ptr(x, None, "x"), _ptr(w_router, dt, "w_router"), _ptr(bias, f32, "bias"), _ptr(wg, dt, "wg"), _ptr(wu, dt, "wu"),
+        _ptr(wd, dt, "wd"), _ptr(addend, dt, "addend"), T, d, E, Ea - E, k, f, dtype_code(dt), _ptr(logits, f32, "logits"),
+        _ptr(topk_idx, torch.int32, "topk_idx"), _ptr(topk_w, f32, "topk_w"), _ptr(out, dt, "out"),
+        _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()), "xmoe_layer_few_fwd")
 
 
 def xmoe_prof_enable(on: bool) -> None:

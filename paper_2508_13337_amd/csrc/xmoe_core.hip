@@ -79,6 +79,11 @@ const char* const kKernelNames[K_COUNT] = {
     "q8_gateup_kernel",
     "q8_rows_kernel",
     "q8_down_kernel",
+    "layer_route_kernel",
+    "layer_up_few_kernel",
+    "layer_down_few_kernel",
+    "layer_up_alu_kernel",
+    "layer_down_alu_kernel",
 };
 
 hipEvent_t get_event() {
@@ -163,6 +168,7 @@ size_t xmoe_workspace_bytes(int op, int rows, int d, int E, int k, int f, int dt
         case XMOE_WS_RBD_STAGE0: return rbd_ws_bytes(rows, k);
         case XMOE_WS_ADD_RMSNORM_BWD: return norm_bwd_ws_bytes(rows, d);
         case XMOE_WS_FFN_Q8_FWD: return ffn_q8_ws_bytes(rows, E, f);
+        case XMOE_WS_LAYER_FEW_FWD: return layer_few_ws_bytes(rows, d, k, f, dt);
         default: return 0;
     }
 }

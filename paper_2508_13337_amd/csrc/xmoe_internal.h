@@ -71,6 +71,11 @@ enum KernelId : int {
     K_Q8_GATEUP,
     K_Q8_ROWS,
     K_Q8_DOWN,
+    K_LAYER_ROUTE,
+    K_LAYER_UP_FEW,
+    K_LAYER_DOWN_FEW,
+    K_LAYER_UP_ALU,
+    K_LAYER_DOWN_ALU,
     K_COUNT
 };
 
