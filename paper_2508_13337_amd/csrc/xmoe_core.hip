@@ -84,6 +84,7 @@ const char* const kKernelNames[K_COUNT] = {
     "layer_down_few_kernel",
     "layer_up_alu_kernel",
     "layer_down_alu_kernel",
+    "layer_sum_kernel",
 };
 
 hipEvent_t get_event() {

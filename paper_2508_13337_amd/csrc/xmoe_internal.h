@@ -76,6 +76,7 @@ enum KernelId : int {
     K_LAYER_DOWN_FEW,
     K_LAYER_UP_ALU,
     K_LAYER_DOWN_ALU,
+    K_LAYER_SUM,
     K_COUNT
 };
 

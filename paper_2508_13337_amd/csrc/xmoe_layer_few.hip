@@ -13,7 +13,7 @@
 //
 // Two families of products: bf16 with widths that are multiples of 64 on the matrix cores (the ring of xmoe_few_tile.h),
 // everything else on the vector ALUs, where 16 groups of threads share a tile's K and read the weights straight to registers.
-#include "xmoe_few_tile.h"
+#include "xmoe_ffn.h"
 #include "xmoe_route.h"
 
 namespace xmoe {
@@ -27,10 +27,9 @@ struct LayerArgs {
     int32_t* topk_idx;
     float* topk_w;
     void* out;
-    int32_t* done;   // [column tiles of down]: blocks that have finished one
     void* act;       // A, one row of f for each (token, expert)
-    float* y;        // the experts' outputs, one row of y_pitch for each (token, expert)
-    int y_pitch;
+    float* y;        // the experts' outputs, slabs x (one row of y_pitch for each (token, expert))
+    int y_pitch, slabs;
 };
 
 // ---------------------------------------------------------------------------------------------------------
@@ -51,13 +50,29 @@ __global__ __launch_bounds__(512) void layer_route_kernel(LayerArgs g) {
     for (int e0 = wave * 8; e0 < g.E; e0 += 64) {
         float p[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (e0 + 8 <= g.E) {
-#pragma unroll 8
-            for (int i = lane; i < g.d; i += 64) {
-                const float a = to_float(x[i]);
-                const LayerVec<T, 8> q = *reinterpret_cast<const LayerVec<T, 8>*>(w + (size_t)i * g.E + e0);
+            // the steps of 64 in which every lane has an element, eight of them with their loads in flight together
+            const int full = g.d / 64;
+            const T *px = x + lane, *pw = w + (size_t)lane * g.E + e0;
+            auto steps = [&](auto n) {
+                constexpr int N = decltype(n)::value;
+                T a[N];
+                LayerVec<T, 8> q[N];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] = fmaf(a, to_float(q.v[j]), p[j]);
-            }
+                for (int u = 0; u < N; ++u) {
+                    a[u] = px[64 * u];
+                    q[u] = *reinterpret_cast<const LayerVec<T, 8>*>(pw + (size_t)(64 * u) * g.E);
+                }
+#pragma unroll
+                for (int u = 0; u < N; ++u)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = fmaf(to_float(a[u]), to_float(q[u].v[j]), p[j]);
+                px += 64 * N;
+                pw += (size_t)(64 * N) * g.E;
+            };
+            int m = 0;
+            for (; m + 8 <= full; m += 8) steps(std::integral_constant<int, 8>{});
+            for (; m < full; ++m) steps(std::integral_constant<int, 1>{});
+            if (64 * full + lane < g.d) steps(std::integral_constant<int, 1>{});
         } else {
             for (int i = lane; i < g.d; i += 64) {
                 const float a = to_float(x[i]);
@@ -102,7 +117,6 @@ struct LayerPlan {
     int wave_sum[4];
     int tok[32];   // the tokens of the block's expert
     int n;         // active experts
-    int last;
 };
 __device__ __forceinline__ uint32_t layer_all(int T) { return T < 32 ? (1u << T) - 1u : ~0u; }
 __device__ __forceinline__ void layer_plan(LayerPlan& pl, const LayerArgs& g) {
@@ -149,128 +163,241 @@ __device__ __forceinline__ int layer_tokens(LayerPlan& pl, int e) {
     return __popc(m);
 }
 
-// The rows of the tokens in columns [n0, n0 + cols) are complete: out = their weighted sum.  Every thread of the last block.
-template <typename T>
-__device__ __forceinline__ void layer_sum(const LayerPlan& pl, const LayerArgs& g, int n0, int cols) {
-    const int groups = cols / 4;   // of four columns
-    for (int i = threadIdx.x; i < g.T * groups; i += 256) {
-        const int t = i / groups, col = n0 + 4 * (i - t * groups);
-        if (col >= g.d) continue;
-        const uint32_t below = (1u << t) - 1u;
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < g.k; ++j) {
-            const int e = g.topk_idx[t * g.k + j];
-            const float w = g.topk_w[t * g.k + j];
-            const float4 v = *reinterpret_cast<const float4*>(g.y + (size_t)(pl.row0[e] + __popc(pl.mask[e] & below)) * g.y_pitch + col);
-            s[0] = fmaf(w, v.x, s[0]);
-            s[1] = fmaf(w, v.y, s[1]);
-            s[2] = fmaf(w, v.z, s[2]);
-            s[3] = fmaf(w, v.w, s[3]);
-        }
-        for (int e = g.E; e < g.E + g.E_s; ++e) {
-            const float4 v = *reinterpret_cast<const float4*>(g.y + (size_t)(pl.row0[e] + t) * g.y_pitch + col);
-            s[0] += v.x;
-            s[1] += v.y;
-            s[2] += v.z;
-            s[3] += v.w;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (col + q < g.d) {
-                const size_t at = (size_t)t * g.d + col + q;
-                ((T*)g.out)[at] = from_float<T>(g.addend ? s[q] + to_float(((const T*)g.addend)[at]) : s[q]);
-            }
-    }
-}
-// Behind the block's rows of y for column tile `tile`: the block that comes last of the n adds the tile up.
-template <typename T>
-__device__ __forceinline__ void layer_finish(LayerPlan& pl, const LayerArgs& g, int tile, int cols) {
-    __threadfence();   // this thread's rows are visible to the device
-    __syncthreads();
-    if (threadIdx.x == 0) pl.last = atomicAdd(&g.done[tile], 1) == pl.n - 1;
-    __syncthreads();
-    if (!pl.last) return;
-    __threadfence();   // and the others' to this block
-    layer_sum<T>(pl, g, tile * cols, cols);
-}
-__device__ __forceinline__ void layer_clear(const LayerArgs& g, int tiles) {
-    if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < tiles; i += 256) g.done[i] = 0;
-}
-
 // ---------------------------------------------------------------------------------------------------------
 // matrix cores (bf16, d % 64 == 0, f % 64 == 0, 16-byte aligned)
 // ---------------------------------------------------------------------------------------------------------
-template <int MODE>
-__device__ __forceinline__ void layer_loader(FewLoader& ld, const bf16_t* x, size_t ldx, const int* tok, int row0, int rows,
-                                             const bf16_t* w0, const bf16_t* w1, int K, int N, int n0) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    {
-        int r = wave * 16 + (lane >> 2);   // rows past the last one repeat it; what they give is not stored
-        const int c = (lane & 3) ^ ((r >> 2) & 3);
-        r = r < rows ? r : rows - 1;
-        ld.x = x + (size_t)(tok ? tok[r] : row0 + r) * ldx + 8 * c;
+// A block of 4 waves multiplies up to 32 rows with COLS columns, 32 k to a stage, on a ring of direct-to-LDS stages.
+// LDS of a stage: 32 k-rows of COLS columns, whose 16-byte pieces are XOR-ed with 4 * (k-row % 4), then 32 rows of x with 64
+// bytes each, pieces XOR-ed with (row / 4) % 4: the fragment reads fall on all banks.
+// The plan lies behind the ring in the same array: LDS reads of an object of its own would make the compiler wait for every
+// direct-to-LDS load in flight at each of the ring's reads.
+typedef __attribute__((ext_vector_type(8))) __bf16 layer_bf16x8_t;
+typedef __attribute__((ext_vector_type(16))) float layer_f32x16_t;
+typedef __attribute__((ext_vector_type(4))) short layer_s16x4_t;
+typedef __attribute__((ext_vector_type(8))) short layer_s16x8_t;
+
+constexpr int kRingK = 32;
+__device__ __forceinline__ void ring_load16(const bf16_t* p, char* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                     (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+// DUAL: the columns are COLS / 2 of two matrices each
+template <int COLS, bool DUAL, int STAGES>
+struct Ring {
+    static constexpr int kW = kRingK * COLS * 2, kStage = kW + 32 * kRingK * 2, kBytes = STAGES * kStage;
+    static constexpr int kLoads = COLS / 64;       // of weights, per wave and stage; waves 0 and 1 fetch a half of x each
+    static constexpr int kBlocks = COLS / 128;     // of 32 columns, per wave
+    static constexpr int kRows = 1024 / (2 * COLS);   // k-rows of a load
+    const bf16_t *w[kLoads], *x;   // of the stage issued next
+    size_t step;                   // elements between the weights of two stages
+    int left;                      // stages behind the one issued next
+
+    // rows: source(r) is row r's element 0; w0, w1: element (first k, n0) of the matrices, N columns of which cols exist
+    template <class Source>
+    __device__ __forceinline__ void init(Source source, int rows, const bf16_t* w0, const bf16_t* w1, int N, int cols,
+                                         int stages) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        {
+            const int r = (wave & 1) * 16 + (lane >> 2), c = (lane & 3) ^ ((r >> 2) & 3);
+            x = source(r < rows ? r : rows - 1) + 8 * c;   // rows past the last one repeat it; what they give is not stored
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int kr = wave * 8 + i * kRows + lane * 8 / COLS;
+            int col = 8 * ((lane & (COLS / 8 - 1)) ^ ((kr & 3) << 2));
+            const bf16_t* b = w0;
+            if (DUAL && col >= COLS / 2) {
+                b = w1;
+                col -= COLS / 2;
+            }
+            if (col >= cols) col = 0;   // past the edge: not stored
+            w[i] = b + (size_t)kr * N + col;
+        }
+        step = (size_t)kRingK * N;
+        left = stages - 1;
     }
-    const int c = (lane & 15) ^ ((lane >> 4) << 2);
-    const bf16_t* w = MODE == FEW_GATEUP && c >= 8 ? w1 : w0;
-    int col = n0 + 8 * (MODE == FEW_GATEUP ? c & 7 : c);
-    if (col >= N) col = n0;   // the second half of a tile at the edge: not stored
-    w += (size_t)(wave * 8 + (lane >> 4)) * N + col;
-    ld.w[0] = w;
-    ld.w[1] = w + (size_t)4 * N;
-    ld.step = (size_t)kFewK * N;
-    ld.left = K / kFewK;
+    // behind the last stage that one is fetched again, so that the counts stay uniform
+    __device__ __forceinline__ void issue(char* __restrict__ stage) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const bool more = left > 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            ring_load16(w[i], stage + wave * (kW / 4) + i * 1024);
+            w[i] += more ? step : 0;
+        }
+        if (wave < 2) ring_load16(x, stage + kW + wave * 1024);
+        x += more ? kRingK : 0;
+        --left;
+    }
+    // at most N stages of the wave's loads on their way, its LDS reads returned
+    template <int N>
+    __device__ __forceinline__ static void wait() {
+        if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 2)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N * (kLoads + 1)) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N * kLoads) : "memory");
+    }
+    // the wave's b-th 32 columns (DUAL with one block: 16 of either matrix), 8 k (16 ks + 8 (lane / 32) ..): in a group of 16
+    // lanes, lane s addresses 4 consecutive columns (s % 4) of k-row s / 4, and the transposing read hands every lane one
+    // column with 4 consecutive k
+    __device__ __forceinline__ static layer_bf16x8_t frag_w(const char* stage, int b, int ks) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = lane >> 4, s = lane & 15;
+        const int col = (DUAL ? (kBlocks == 1 ? 64 * (G & 1) + 16 * wave : 128 * b + 32 * wave + 16 * (G & 1))
+                              : 32 * kBlocks * wave + 32 * b + 16 * (G & 1)) + 4 * (s & 3);
+        layer_s16x4_t h[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int kr = 16 * ks + 8 * (G >> 1) + (s >> 2) + 4 * q;
+            const char* a = stage + kr * (2 * COLS) + (((col >> 3) ^ ((kr & 3) << 2)) << 4) + (col & 7) * 2;
+            h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) layer_s16x4_t*)(
+                (__attribute__((address_space(3))) void*)a));
+        }
+        const layer_s16x8_t v = {h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]};
+        return __builtin_bit_cast(layer_bf16x8_t, v);
+    }
+    __device__ __forceinline__ static layer_bf16x8_t frag_x(const char* stage, int ks) {
+        const int lane = threadIdx.x & 63, r = lane & 31, c = 2 * ks + (lane >> 5);
+        return *reinterpret_cast<const layer_bf16x8_t*>(stage + kW + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+    }
+    // Refills the stage read before the last barrier and multiplies `cur`.  The two are distinct, and saying so matters: an
+    // LDS read that may observe a direct-to-LDS load in flight makes the compiler wait for all of them.
+    __device__ __forceinline__ void step_on(layer_f32x16_t (&acc)[kBlocks], char* __restrict__ next,
+                                            const char* __restrict__ cur) {
+        issue(next);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const layer_bf16x8_t a = frag_x(cur, ks);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_w(cur, b, ks), a, acc[b], 0, 0, 0);
+        }
+    }
+    // acc[b], register v of lane l: row l % 32, column 8 (v/4) + 4 (l/32) + v%4 of the wave's b-th 32
+    __device__ __forceinline__ void run(layer_f32x16_t (&acc)[kBlocks], char* smem, int stages) {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[b][v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) issue(smem + s * kStage);
+        int cur = 0, next = STAGES - 1;
+        for (int i = 0; i < stages; ++i) {
+            // stage i has landed for every thread, and every wave is done with stage i - 1, which is refilled now
+            wait<STAGES - 2>();
+            asm volatile("s_barrier" ::: "memory");
+            step_on(acc, smem + next * kStage, smem + cur * kStage);
+            next = cur;
+            cur = cur + 1 < STAGES ? cur + 1 : 0;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land in this LDS once the block has left it
+    }
+};
+
+__device__ __forceinline__ void layer_store_act(const LayerArgs& g, int row, int col, const float (&gv)[4], const float (&uv)[4]) {
+    float a[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = gv[i] * fast_sigmoid(gv[i]) * uv[i];
+    *reinterpret_cast<uint2*>((bf16_t*)g.act + (size_t)row * g.f + col) = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]));
 }
 
-__global__ __launch_bounds__(256, 2) void layer_up_few_kernel(LayerArgs g, int down_tiles) {
-    __shared__ __align__(16) char smem[kFewStages * kFewStageBytes];
-    __shared__ LayerPlan pl;
-    layer_clear(g, down_tiles);
+// COLS / 2 columns of A of one expert
+template <int COLS, int STAGES>
+__global__ __launch_bounds__(256, 2) void layer_up_few_kernel(LayerArgs g) {
+    typedef Ring<COLS, true, STAGES> R;
+    __shared__ __align__(16) char smem[R::kBytes + sizeof(LayerPlan)];
+    LayerPlan& pl = *reinterpret_cast<LayerPlan*>(smem + R::kBytes);
     layer_plan(pl, g);
-    const int nt = (g.f + 63) / 64, i = blockIdx.x / nt, n0 = (blockIdx.x - i * nt) * 64;
+    const int nt = (g.f + COLS / 2 - 1) / (COLS / 2), i = blockIdx.x / nt, n0 = (blockIdx.x - i * nt) * (COLS / 2);
     if (i >= pl.n) return;
-    const int e = pl.list[i], rows = layer_tokens(pl, e);
-    const size_t we = (size_t)e * g.d * g.f;
-    FewLoader ld;
-    layer_loader<FEW_GATEUP>(ld, (const bf16_t*)g.x, g.d, pl.tok, 0, rows, (const bf16_t*)g.wg + we, (const bf16_t*)g.wu + we,
-                             g.d, g.f, n0);
-    few_f32x16_t acc[1];
-    few_loop<FEW_GATEUP, 1>(acc, ld, smem, g.d / kFewK);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, col = n0 + 16 * wave + 4 * (lane >> 5);
+    const int e = pl.list[i], rows = layer_tokens(pl, e), row0 = pl.row0[e];
+    const size_t we = (size_t)e * g.d * g.f + n0;
+    R ring;
+    ring.init([&](int r) { return (const bf16_t*)g.x + (size_t)pl.tok[r] * g.d; }, rows, (const bf16_t*)g.wg + we,
+              (const bf16_t*)g.wu + we, g.f, g.f - n0, g.d / kRingK);
+    layer_f32x16_t acc[R::kBlocks];
+    ring.run(acc, smem, g.d / kRingK);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31;
     if (r >= rows) return;
-    bf16_t* o = (bf16_t*)g.act + (size_t)(pl.row0[e] + r) * g.f + col;
+    const int col = n0 + COLS / 8 * wave + 4 * (lane >> 5);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        float a[4];
+    for (int q = 0; q < COLS / 64; ++q) {
+        float gv[4], uv[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const float gv = acc[0][4 * q + v];
-            a[v] = gv * fast_sigmoid(gv) * acc[0][8 + 4 * q + v];
+            gv[v] = acc[0][4 * q + v];
+            uv[v] = COLS == 128 ? acc[0][(8 + 4 * q + v) & 15] : acc[R::kBlocks - 1][4 * q + v];
         }
-        *reinterpret_cast<uint2*>(o + 8 * q) = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]));
+        if (col + 8 * q < g.f) layer_store_act(g, row0 + r, col + 8 * q, gv, uv);
     }
 }
 
+// 256 columns of an expert's output, over a slab of f
+constexpr int kDownCols = 256, kDownStages = 4;
 __global__ __launch_bounds__(256, 2) void layer_down_few_kernel(LayerArgs g) {
-    __shared__ __align__(16) char smem[kFewStages * kFewStageBytes];
-    __shared__ LayerPlan pl;
+    typedef Ring<kDownCols, false, kDownStages> R;
+    __shared__ __align__(16) char smem[R::kBytes + sizeof(LayerPlan)];
+    LayerPlan& pl = *reinterpret_cast<LayerPlan*>(smem + R::kBytes);
     layer_plan(pl, g);
-    const int nt = (g.d + kFewCols - 1) / kFewCols, i = blockIdx.x / nt, tile = blockIdx.x - i * nt, n0 = tile * kFewCols;
+    const int nt = (g.d + kDownCols - 1) / kDownCols, per = nt * g.slabs, i = blockIdx.x / per;
     if (i >= pl.n) return;
+    const int slab = (blockIdx.x - i * per) / nt, n0 = (blockIdx.x - i * per - slab * nt) * kDownCols;
+    const int all = g.f / kRingK, s0 = all * slab / g.slabs, s1 = all * (slab + 1) / g.slabs;   // slabs <= all
     const int e = pl.list[i], rows = __popc(pl.mask[e]), row0 = pl.row0[e];
-    FewLoader ld;
-    layer_loader<FEW_PLAIN>(ld, (const bf16_t*)g.act, g.f, nullptr, row0, rows, (const bf16_t*)g.wd + (size_t)e * g.f * g.d,
-                            nullptr, g.f, g.d, n0);
-    few_f32x16_t acc[1];
-    few_loop<FEW_PLAIN, 1>(acc, ld, smem, g.f / kFewK);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, col = n0 + 32 * wave + 4 * (lane >> 5);
-    if (r < rows && col < g.d) {
-        float* o = g.y + (size_t)(row0 + r) * g.y_pitch + col;
+    R ring;
+    ring.init([&](int r) { return (const bf16_t*)g.act + (size_t)(row0 + r) * g.f + s0 * kRingK; }, rows,
+              (const bf16_t*)g.wd + ((size_t)e * g.f + s0 * kRingK) * g.d + n0, nullptr, g.d, g.d - n0, s1 - s0);
+    layer_f32x16_t acc[R::kBlocks];
+    ring.run(acc, smem, s1 - s0);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31;
+    if (r >= rows) return;
+    const int col = n0 + 64 * wave + 4 * (lane >> 5);
+    float* o = g.y + ((size_t)slab * g.T * (g.k + g.E_s) + row0 + r) * g.y_pitch + col;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<float4*>(o + 8 * q) = make_float4(acc[0][4 * q], acc[0][4 * q + 1], acc[0][4 * q + 2], acc[0][4 * q + 3]);
+            if (col + 32 * b + 8 * q < g.d)
+                *reinterpret_cast<float4*>(o + 32 * b + 8 * q) =
+                    make_float4(acc[b][4 * q], acc[b][4 * q + 1], acc[b][4 * q + 2], acc[b][4 * q + 3]);
+}
+
+// out = the weighted sum of the tokens' rows: slots in order, then the shared experts, then the addend; a row's slabs in order.
+// One block per token and 1024 columns.
+template <typename T>
+__global__ __launch_bounds__(256) void layer_sum_kernel(LayerArgs g) {
+    __shared__ LayerPlan pl;
+    layer_plan(pl, g);
+    const int t = blockIdx.x, col = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (col >= g.d) return;
+    const uint32_t below = (1u << t) - 1u;
+    const size_t slab = (size_t)g.T * (g.k + g.E_s) * g.y_pitch;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < g.k + g.E_s; ++j) {
+        const int e = j < g.k ? g.topk_idx[t * g.k + j] : g.E + j - g.k;
+        const float w = j < g.k ? g.topk_w[t * g.k + j] : 1.0f;
+        const float* p = g.y + (size_t)(pl.row0[e] + __popc(pl.mask[e] & below)) * g.y_pitch + col;
+        float4 v = *reinterpret_cast<const float4*>(p);
+        for (int i = 1; i < g.slabs; ++i) {
+            const float4 q = *reinterpret_cast<const float4*>(p + i * slab);
+            v = make_float4(v.x + q.x, v.y + q.y, v.z + q.z, v.w + q.w);
+        }
+        s[0] = fmaf(w, v.x, s[0]);
+        s[1] = fmaf(w, v.y, s[1]);
+        s[2] = fmaf(w, v.z, s[2]);
+        s[3] = fmaf(w, v.w, s[3]);
     }
-    layer_finish<bf16_t>(pl, g, tile, kFewCols);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (col + q < g.d) {
+            const size_t at = (size_t)t * g.d + col + q;
+            ((T*)g.out)[at] = from_float<T>(g.addend ? s[q] + to_float(((const T*)g.addend)[at]) : s[q]);
+        }
+}
+template <typename T>
+int launch_layer_sum(const LayerArgs& a, hipStream_t s) {
+    XMOE_LAUNCH(K_LAYER_SUM, s, hipLaunchKernelGGL(layer_sum_kernel<T>, dim3((unsigned)a.T, (unsigned)((a.d + 1023) / 1024)),
+                                                   dim3(256), 0, s, a));
+    return XMOE_OK;
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -379,11 +506,10 @@ __device__ __forceinline__ void alu_product(const T* x, size_t ldx, int rows, in
 }
 
 template <typename T, int EV>
-__global__ __launch_bounds__(256) void layer_up_alu_kernel(LayerArgs g, int down_tiles) {
+__global__ __launch_bounds__(256) void layer_up_alu_kernel(LayerArgs g) {
     constexpr int C = 16 * EV;
     __shared__ float red[4 * 2 * kAluRows * C];
     __shared__ LayerPlan pl;
-    layer_clear(g, down_tiles);
     layer_plan(pl, g);
     const int nt = (g.f + C - 1) / C, i = blockIdx.x / nt, n0 = (blockIdx.x - i * nt) * C;
     if (i >= pl.n) return;
@@ -408,7 +534,6 @@ __global__ __launch_bounds__(256) void layer_down_alu_kernel(LayerArgs g) {
     alu_product<T, 1, EV>((const T*)g.act, g.f, rows, g.f, (const T*)g.wd + (size_t)e * g.f * g.d, (const T*)nullptr, g.d,
                             tile * C, red, [&](int r) { return row0 + r; },
                             [&](int r, int c, float v, float) { g.y[(size_t)(row0 + r) * g.y_pitch + c] = v; });
-    layer_finish<T>(pl, g, tile, C);
 }
 
 template <typename T>
@@ -417,14 +542,14 @@ int launch_alu(const LayerArgs& a, int active, hipStream_t s) {
     const int cu = a.f < EV ? 16 : 16 * EV, cd = a.d < EV ? 16 : 16 * EV, up = (a.f + cu - 1) / cu, down = (a.d + cd - 1) / cd;
     const dim3 g1((unsigned)(active * up)), g2((unsigned)(active * down));
     if (a.f < EV)
-        XMOE_LAUNCH(K_LAYER_UP_ALU, s, hipLaunchKernelGGL((layer_up_alu_kernel<T, 1>), g1, dim3(256), 0, s, a, down));
+        XMOE_LAUNCH(K_LAYER_UP_ALU, s, hipLaunchKernelGGL((layer_up_alu_kernel<T, 1>), g1, dim3(256), 0, s, a));
     else
-        XMOE_LAUNCH(K_LAYER_UP_ALU, s, hipLaunchKernelGGL((layer_up_alu_kernel<T, EV>), g1, dim3(256), 0, s, a, down));
+        XMOE_LAUNCH(K_LAYER_UP_ALU, s, hipLaunchKernelGGL((layer_up_alu_kernel<T, EV>), g1, dim3(256), 0, s, a));
     if (a.d < EV)
         XMOE_LAUNCH(K_LAYER_DOWN_ALU, s, hipLaunchKernelGGL((layer_down_alu_kernel<T, 1>), g2, dim3(256), 0, s, a));
     else
         XMOE_LAUNCH(K_LAYER_DOWN_ALU, s, hipLaunchKernelGGL((layer_down_alu_kernel<T, EV>), g2, dim3(256), 0, s, a));
-    return XMOE_OK;
+    return launch_layer_sum<T>(a, s);
 }
 
 template <typename T>
@@ -442,6 +567,8 @@ int launch_layer_route(const LayerArgs& a, hipStream_t s) {
 
 // A block per token reads the whole router: up to this many bytes of it
 constexpr size_t kRouteBytes = 512 << 10;
+// From this many tiles of 128 columns on, up takes them (rows of 256 bytes of either matrix) instead of 64
+constexpr long kWideTiles = 400;
 
 }  // namespace
 }  // namespace xmoe
@@ -465,13 +592,10 @@ extern "C" int xmoe_layer_few_fwd(const void* x, const void* w_router, const flo
     hipStream_t s = (hipStream_t)stream;
     const size_t rows = (size_t)T * (k + E_s);
     LayerArgs a{x, w_router, wg, wu, wd, addend, bias, T, d, E, E_s, k, f, logits, topk_idx, topk_w, out};
-    char* p = (char*)ws;
-    a.done = (int32_t*)p;
-    p += layer_few_done_bytes(d);
-    a.act = p;
-    p += align_up(rows * f * dtype_size(dt), 256);
-    a.y = (float*)p;
+    a.slabs = 1;
     a.y_pitch = layer_few_y_pitch(d);
+    a.act = ws;
+    a.y = (float*)((char*)ws + align_up(rows * f * dtype_size(dt), 256));
     int st;
     if ((size_t)d * E * dtype_size(dt) <= kRouteBytes) {
         st = dt == XMOE_F32 ? launch_layer_route<float>(a, s) : launch_layer_route<bf16_t>(a, s);
@@ -484,10 +608,17 @@ extern "C" int xmoe_layer_few_fwd(const void* x, const void* w_router, const flo
     if (dt == XMOE_F32) return launch_alu<float>(a, active, s);
     if (d % 64 || f % 64 || !aligned16(x) || !aligned16(wg) || !aligned16(wu) || !aligned16(wd))
         return launch_alu<bf16_t>(a, active, s);
-    const int up = f / 64, down = (d + kFewCols - 1) / kFewCols;
-    XMOE_LAUNCH(K_LAYER_UP_FEW, s,
-                hipLaunchKernelGGL(layer_up_few_kernel, dim3((unsigned)(active * up)), dim3(256), 0, s, a, down));
-    XMOE_LAUNCH(K_LAYER_DOWN_FEW, s,
-                hipLaunchKernelGGL(layer_down_few_kernel, dim3((unsigned)(active * down)), dim3(256), 0, s, a));
-    return XMOE_OK;
+    // slabs of at least 8 stages until a token's experts alone give two blocks to every CU (the number of tokens has no say:
+    // a token's bits are the same in every call)
+    int down = (d + kDownCols - 1) / kDownCols;
+    while (a.slabs < kLayerSlabs && (k + E_s) * down * a.slabs < 512 && f / kRingK >= 8 * (a.slabs + 1)) ++a.slabs;
+    down *= a.slabs;
+    if ((long)active * ((f + 127) / 128) >= kWideTiles)
+        XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<256, 4>), dim3((unsigned)(active * ((f + 127) / 128))),
+                                                          dim3(256), 0, s, a));
+    else
+        XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<128, 6>), dim3((unsigned)(active * (f / 64))),
+                                                          dim3(256), 0, s, a));
+    XMOE_LAUNCH(K_LAYER_DOWN_FEW, s, hipLaunchKernelGGL(layer_down_few_kernel, dim3((unsigned)(active * down)), dim3(256), 0, s, a));
+    return launch_layer_sum<bf16_t>(a, s);
 }
