@@ -29,69 +29,114 @@ struct LayerArgs {
     void* out;
     void* act;       // A, one row of f for each (token, expert)
     float* y;        // the experts' outputs, slabs x (one row of y_pitch for each (token, expert))
+    int32_t* row_of;   // [T][k + E_s]: the row of a token's j-th expert
     int y_pitch, slabs;
 };
 
 // ---------------------------------------------------------------------------------------------------------
-// route: one block of 8 waves per token.  Wave w takes the experts 8 w .., 8 (w + 8) ..
+// route: one block of 8 waves per token.  Wave w takes the experts 8 w .., 8 (w + 8) ..; lane l is the partial sum l.
+// The router's rows are contiguous, and a lane wants 16 bytes of a row of its own: a stage of whole rows goes through LDS (rows
+// 16 bytes further apart than in memory, which keeps the lanes off each other's banks), the next one is on its way in
+// registers.  Straight from memory every wave would touch every line of the router.
 // ---------------------------------------------------------------------------------------------------------
 // elements at an address that is aligned to one
 template <typename T, int N>
 struct __attribute__((packed, aligned(sizeof(T)))) LayerVec {
     T v[N];
 };
+constexpr int kRouteLds = 64 << 10, kRoutePieces = 8;   // of 16 bytes, per thread and stage: 512 * 8 of them are a stage's most
+constexpr int kRouteSteps = 32;                         // of 64 rows: a stage's most
 
+// pitch: bytes of a staged row, 0: rows that are no whole 16-byte pieces are read from memory
 template <typename T, int PER_LANE>
-__global__ __launch_bounds__(512) void layer_route_kernel(LayerArgs g) {
-    __shared__ float row[XMOE_MAX_EXPERTS];
+__global__ __launch_bounds__(512) void layer_route_kernel(LayerArgs g, int pitch, int steps) {
+    __shared__ __align__(16) char stage[kRouteLds];
+    __shared__ float row[XMOE_MAX_EXPERTS], xs[64 * kRouteSteps];
     const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const T* x = (const T*)g.x + (size_t)t * g.d;
     const T* w = (const T*)g.w_router;
-    for (int e0 = wave * 8; e0 < g.E; e0 += 64) {
-        float p[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (e0 + 8 <= g.E) {
-            // the steps of 64 in which every lane has an element, eight of them with their loads in flight together
-            const int full = g.d / 64;
-            const T *px = x + lane, *pw = w + (size_t)lane * g.E + e0;
-            auto steps = [&](auto n) {
-                constexpr int N = decltype(n)::value;
-                T a[N];
-                LayerVec<T, 8> q[N];
+    float p[PER_LANE][8];
 #pragma unroll
-                for (int u = 0; u < N; ++u) {
-                    a[u] = px[64 * u];
-                    q[u] = *reinterpret_cast<const LayerVec<T, 8>*>(pw + (size_t)(64 * u) * g.E);
+    for (int h = 0; h < PER_LANE; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[h][j] = 0.f;
+    if (pitch) {
+        const int per_row = pitch / 16 - 1, stage_rows = 64 * steps;
+        const uint4* src = reinterpret_cast<const uint4*>(w);
+        int at[kRoutePieces];   // LDS addresses of the thread's pieces
+        uint4 v[kRoutePieces];
+        T xv[kRouteSteps / 8];
+#pragma unroll
+        for (int u = 0; u < kRoutePieces; ++u) {
+            const int n = threadIdx.x + 512 * u, r = n / per_row;
+            at[u] = r < stage_rows ? r * pitch + (n - r * per_row) * 16 : -1;
+        }
+        auto fetch = [&](int row0) {
+            const int n_valid = (g.d - row0) * per_row;   // pieces left
+#pragma unroll
+            for (int u = 0; u < kRoutePieces; ++u) {
+                const int n = threadIdx.x + 512 * u;
+                v[u] = at[u] >= 0 && n < n_valid ? src[(size_t)row0 * per_row + n] : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int u = 0; u < kRouteSteps / 8; ++u) {
+                const int n = row0 + threadIdx.x + 512 * u;
+                xv[u] = x[n < g.d ? n : g.d - 1];
+            }
+        };
+        fetch(0);
+        for (int row0 = 0; row0 < g.d; row0 += stage_rows) {
+            __syncthreads();   // the last stage has been read
+#pragma unroll
+            for (int u = 0; u < kRoutePieces; ++u)
+                if (at[u] >= 0) *reinterpret_cast<uint4*>(stage + at[u]) = v[u];
+#pragma unroll
+            for (int u = 0; u < kRouteSteps / 8; ++u) xs[threadIdx.x + 512 * u] = to_float(xv[u]);
+            __syncthreads();
+            if (row0 + stage_rows < g.d) fetch(row0 + stage_rows);
+            for (int s = 0; s < steps; ++s) {
+                const int i = row0 + 64 * s + lane;
+                if (i >= g.d) break;
+                const float a = xs[64 * s + lane];
+                const char* r = stage + (64 * s + lane) * pitch;
+#pragma unroll
+                for (int h = 0; h < PER_LANE; ++h) {
+                    const int e0 = 8 * wave + 64 * h;
+                    if (e0 < g.E) {
+                        const LayerVec<T, 8> q = *reinterpret_cast<const LayerVec<T, 8>*>(r + e0 * (int)sizeof(T));
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) p[h][j] = fmaf(a, to_float(q.v[j]), p[h][j]);
+                    }
                 }
-#pragma unroll
-                for (int u = 0; u < N; ++u)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) p[j] = fmaf(to_float(a[u]), to_float(q[u].v[j]), p[j]);
-                px += 64 * N;
-                pw += (size_t)(64 * N) * g.E;
-            };
-            int m = 0;
-            for (; m + 8 <= full; m += 8) steps(std::integral_constant<int, 8>{});
-            for (; m < full; ++m) steps(std::integral_constant<int, 1>{});
-            if (64 * full + lane < g.d) steps(std::integral_constant<int, 1>{});
-        } else {
-            for (int i = lane; i < g.d; i += 64) {
-                const float a = to_float(x[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (e0 + j < g.E) p[j] = fmaf(a, to_float(w[(size_t)i * g.E + e0 + j]), p[j]);
             }
         }
+    } else {
+        for (int i = lane; i < g.d; i += 64) {
+            const float a = to_float(x[i]);
+#pragma unroll
+            for (int h = 0; h < PER_LANE; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int e = 8 * wave + 64 * h + j;
+                    if (e < g.E) p[h][j] = fmaf(a, to_float(w[(size_t)i * g.E + e]), p[h][j]);
+                }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < PER_LANE; ++h) {
+        const int e0 = 8 * wave + 64 * h;
+        if (e0 >= g.E) break;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] += __shfl_xor(p[j], off, 64);
+            for (int j = 0; j < 8; ++j) p[h][j] += __shfl_xor(p[h][j], off, 64);
         if (lane == 0) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (e0 + j < g.E) {
-                    const float v = g.bias ? p[j] + g.bias[e0 + j] : p[j];
-                    row[e0 + j] = v;
-                    g.logits[(size_t)t * g.E + e0 + j] = v;
+                    const float l = g.bias ? p[h][j] + g.bias[e0 + j] : p[h][j];
+                    row[e0 + j] = l;
+                    g.logits[(size_t)t * g.E + e0 + j] = l;
                 }
         }
     }
@@ -154,6 +199,14 @@ __device__ __forceinline__ void layer_plan(LayerPlan& pl, const LayerArgs& g) {
     if (m1) pl.list[at] = 2 * tid + 1;
     if (tid == 0) pl.n = all & 0xffff;
     __syncthreads();
+}
+// the rows of the tokens' experts, for the sums (by one block of up)
+__device__ __forceinline__ void layer_rows(const LayerPlan& pl, const LayerArgs& g) {
+    const int n = g.k + g.E_s;
+    for (int i = threadIdx.x; i < g.T * n; i += 256) {
+        const int t = i / n, j = i - t * n, e = j < g.k ? g.topk_idx[t * g.k + j] : g.E + j - g.k;
+        g.row_of[i] = pl.row0[e] + __popc(pl.mask[e] & ((1u << t) - 1u));
+    }
 }
 // the block's expert (of the plan's list), its tokens in pl.tok; returns how many
 __device__ __forceinline__ int layer_tokens(LayerPlan& pl, int e) {
@@ -307,6 +360,7 @@ __global__ __launch_bounds__(256, 2) void layer_up_few_kernel(LayerArgs g) {
     __shared__ __align__(16) char smem[R::kBytes + sizeof(LayerPlan)];
     LayerPlan& pl = *reinterpret_cast<LayerPlan*>(smem + R::kBytes);
     layer_plan(pl, g);
+    if (blockIdx.x == 0) layer_rows(pl, g);
     const int nt = (g.f + COLS / 2 - 1) / (COLS / 2), i = blockIdx.x / nt, n0 = (blockIdx.x - i * nt) * (COLS / 2);
     if (i >= pl.n) return;
     const int e = pl.list[i], rows = layer_tokens(pl, e), row0 = pl.row0[e];
@@ -362,29 +416,37 @@ __global__ __launch_bounds__(256, 2) void layer_down_few_kernel(LayerArgs g) {
 }
 
 // out = the weighted sum of the tokens' rows: slots in order, then the shared experts, then the addend; a row's slabs in order.
-// One block per token and 1024 columns.
-template <typename T>
+// Latency: a thread's rows are fetched eight at a time.  One block per token and 1024 columns.
+template <typename T, int SLABS>
 __global__ __launch_bounds__(256) void layer_sum_kernel(LayerArgs g) {
-    __shared__ LayerPlan pl;
-    layer_plan(pl, g);
-    const int t = blockIdx.x, col = (blockIdx.y * 256 + threadIdx.x) * 4;
+    const int t = blockIdx.x, col = (blockIdx.y * 256 + threadIdx.x) * 4, n = g.k + g.E_s;
     if (col >= g.d) return;
-    const uint32_t below = (1u << t) - 1u;
-    const size_t slab = (size_t)g.T * (g.k + g.E_s) * g.y_pitch;
+    const size_t slab = (size_t)g.T * n * g.y_pitch;
+    constexpr int N = 8 / SLABS;   // rows at a time
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < g.k + g.E_s; ++j) {
-        const int e = j < g.k ? g.topk_idx[t * g.k + j] : g.E + j - g.k;
-        const float w = j < g.k ? g.topk_w[t * g.k + j] : 1.0f;
-        const float* p = g.y + (size_t)(pl.row0[e] + __popc(pl.mask[e] & below)) * g.y_pitch + col;
-        float4 v = *reinterpret_cast<const float4*>(p);
-        for (int i = 1; i < g.slabs; ++i) {
-            const float4 q = *reinterpret_cast<const float4*>(p + i * slab);
-            v = make_float4(v.x + q.x, v.y + q.y, v.z + q.z, v.w + q.w);
+    for (int j0 = 0; j0 < n; j0 += N) {
+        float4 v[N][SLABS];
+        float w[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int j = j0 + u < n ? j0 + u : n - 1;   // past the last one: fetched again, not added
+            const float* p = g.y + (size_t)g.row_of[t * n + j] * g.y_pitch + col;
+            w[u] = j < g.k ? g.topk_w[t * g.k + j] : 1.0f;
+#pragma unroll
+            for (int i = 0; i < SLABS; ++i) v[u][i] = *reinterpret_cast<const float4*>(p + i * slab);
         }
-        s[0] = fmaf(w, v.x, s[0]);
-        s[1] = fmaf(w, v.y, s[1]);
-        s[2] = fmaf(w, v.z, s[2]);
-        s[3] = fmaf(w, v.w, s[3]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (j0 + u >= n) break;
+            float4 a = v[u][0];
+#pragma unroll
+            for (int i = 1; i < SLABS; ++i)
+                a = make_float4(a.x + v[u][i].x, a.y + v[u][i].y, a.z + v[u][i].z, a.w + v[u][i].w);
+            s[0] = fmaf(w[u], a.x, s[0]);
+            s[1] = fmaf(w[u], a.y, s[1]);
+            s[2] = fmaf(w[u], a.z, s[2]);
+            s[3] = fmaf(w[u], a.w, s[3]);
+        }
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -395,8 +457,12 @@ __global__ __launch_bounds__(256) void layer_sum_kernel(LayerArgs g) {
 }
 template <typename T>
 int launch_layer_sum(const LayerArgs& a, hipStream_t s) {
-    XMOE_LAUNCH(K_LAYER_SUM, s, hipLaunchKernelGGL(layer_sum_kernel<T>, dim3((unsigned)a.T, (unsigned)((a.d + 1023) / 1024)),
-                                                   dim3(256), 0, s, a));
+    const dim3 grid((unsigned)a.T, (unsigned)((a.d + 1023) / 1024));
+#define XMOE_CALL(N) XMOE_LAUNCH(K_LAYER_SUM, s, hipLaunchKernelGGL((layer_sum_kernel<T, N>), grid, dim3(256), 0, s, a))
+    if (a.slabs == 1) XMOE_CALL(1);
+    else if (a.slabs == 2) XMOE_CALL(2);
+    else XMOE_CALL(4);
+#undef XMOE_CALL
     return XMOE_OK;
 }
 
@@ -511,6 +577,7 @@ __global__ __launch_bounds__(256) void layer_up_alu_kernel(LayerArgs g) {
     __shared__ float red[4 * 2 * kAluRows * C];
     __shared__ LayerPlan pl;
     layer_plan(pl, g);
+    if (blockIdx.x == 0) layer_rows(pl, g);
     const int nt = (g.f + C - 1) / C, i = blockIdx.x / nt, n0 = (blockIdx.x - i * nt) * C;
     if (i >= pl.n) return;
     const int e = pl.list[i], rows = layer_tokens(pl, e), row0 = pl.row0[e];
@@ -555,8 +622,14 @@ int launch_alu(const LayerArgs& a, int active, hipStream_t s) {
 template <typename T>
 int launch_layer_route(const LayerArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)a.T);
+    const int row_bytes = a.E * (int)sizeof(T);
+    int pitch = row_bytes + 16;
+    // rows of a stage: what LDS and 512 * kRoutePieces pieces hold, in steps of 64.  An expert's eight are whole pieces too.
+    int steps = kRouteLds / (64 * pitch) < kRouteSteps ? kRouteLds / (64 * pitch) : kRouteSteps;
+    while (steps > 1 && steps * 64 * (row_bytes / 16) > 512 * kRoutePieces) --steps;
+    if (a.E % 8 || !aligned16(a.w_router) || steps < 1 || steps * 64 * (row_bytes / 16) > 512 * kRoutePieces) pitch = 0;
 #define XMOE_CALL(PL) \
-    XMOE_LAUNCH(K_LAYER_ROUTE, s, hipLaunchKernelGGL((layer_route_kernel<T, PL>), grid, dim3(512), 0, s, a))
+    XMOE_LAUNCH(K_LAYER_ROUTE, s, hipLaunchKernelGGL((layer_route_kernel<T, PL>), grid, dim3(512), 0, s, a, pitch, steps))
     if (a.E <= 64) XMOE_CALL(1);
     else if (a.E <= 128) XMOE_CALL(2);
     else if (a.E <= 256) XMOE_CALL(4);
@@ -594,8 +667,12 @@ extern "C" int xmoe_layer_few_fwd(const void* x, const void* w_router, const flo
     LayerArgs a{x, w_router, wg, wu, wd, addend, bias, T, d, E, E_s, k, f, logits, topk_idx, topk_w, out};
     a.slabs = 1;
     a.y_pitch = layer_few_y_pitch(d);
-    a.act = ws;
-    a.y = (float*)((char*)ws + align_up(rows * f * dtype_size(dt), 256));
+    char* p = (char*)ws;
+    a.row_of = (int32_t*)p;
+    p += align_up(rows * sizeof(int32_t), 256);
+    a.act = p;
+    p += align_up(rows * f * dtype_size(dt), 256);
+    a.y = (float*)p;
     int st;
     if ((size_t)d * E * dtype_size(dt) <= kRouteBytes) {
         st = dt == XMOE_F32 ? launch_layer_route<float>(a, s) : launch_layer_route<bf16_t>(a, s);
@@ -611,7 +688,7 @@ extern "C" int xmoe_layer_few_fwd(const void* x, const void* w_router, const flo
     // slabs of at least 8 stages until a token's experts alone give two blocks to every CU (the number of tokens has no say:
     // a token's bits are the same in every call)
     int down = (d + kDownCols - 1) / kDownCols;
-    while (a.slabs < kLayerSlabs && (k + E_s) * down * a.slabs < 512 && f / kRingK >= 8 * (a.slabs + 1)) ++a.slabs;
+    while (a.slabs < kLayerSlabs && (k + E_s) * down * a.slabs < 512 && f / kRingK >= 16 * a.slabs) a.slabs *= 2;
     down *= a.slabs;
     if ((long)active * ((f + 127) / 128) >= kWideTiles)
         XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<256, 4>), dim3((unsigned)(active * ((f + 127) / 128))),

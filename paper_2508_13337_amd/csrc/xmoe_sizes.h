@@ -92,13 +92,14 @@ static inline size_t ffn_q8_ws_bytes(int B, int E, int f) {
            align_up(b * 4, 256);
 }
 
-// ----- a layer for a few tokens: A | the experts' outputs in float32; one row for each (token, expert), `slots` experts per
+// ----- a layer for a few tokens: row numbers | A | the experts' outputs in float32; one row for each (token, expert), `slots` experts per
 // token.  The outputs are sums over up to kLayerSlabs slabs of f, a copy of the rows for each -----
 constexpr int kLayerSlabs = 4;
 static inline int layer_few_y_pitch(int d) { return (d + 3) / 4 * 4; }
 static inline size_t layer_few_ws_bytes(int T, int d, int slots, int f, int dt) {
     const size_t rows = (size_t)(T > 0 ? T : 1) * (size_t)(slots > 0 ? slots : 1);
-    return align_up(rows * f * dtype_size(dt), 256) + align_up(rows * layer_few_y_pitch(d) * 4 * kLayerSlabs, 256);
+    return align_up(rows * sizeof(int32_t), 256) + align_up(rows * f * dtype_size(dt), 256) +
+           align_up(rows * layer_few_y_pitch(d) * 4 * kLayerSlabs, 256);
 }
 
 // ----- norm backward: one partial row of dgain per block (two blocks per CU) -----
