@@ -68,19 +68,10 @@ __device__ __forceinline__ q8_i32x4_t q8_frag(const char* unit, int base, int ks
 
 // The weights come first in the instruction: accumulator register v of lane l is row l % 32 and column
 // 8 (v / 4) + 4 (l / 32) + v % 4 of its 32 x 32 block.
-template <int MI>
+template <int MI, int NI>
 struct Q8Frags {
-    q8_i32x4_t a[MI], b[2];
+    q8_i32x4_t a[MI], b[NI];
 };
-template <int MI>
-__device__ __forceinline__ void q8_mma(q8_i32x16_t (&acc)[MI][2], const Q8Frags<MI>& f) {
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-        for (int ni = 0; ni < 2; ++ni)
-            acc[mi][ni] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.b[ni], f.a[mi], acc[mi][ni], 0, 0, 0);
-}
-
 // four values from an address that is aligned to one
 struct __attribute__((packed, aligned(4))) Q8F4 {
     float v[4];
@@ -95,37 +86,31 @@ __device__ __forceinline__ void q8_scales(const float* __restrict__ scale, int c
         for (int i = 0; i < 4; ++i) s[i] = col + i < N ? scale[col + i] : 0.f;   // columns past N: zero
     }
 }
-__device__ __forceinline__ int q8_round16(float v, float inv) {
-    return (int)rintf(fminf(fmaxf(v * inv, -32767.f), 32767.f));
-}
-
 // A row's 32 columns of gate and up sums (this lane: 16 of them) -> 16-bit integers, packed in the order of the registers'
-// column quadruples, and the maximum of all 32.  gs, us: the columns' scales
+// column quadruples, and the maximum of all 32.  gs: the gate columns' scales times log2 e, us: the up columns' divided by
+// it.  The row's scale is a factor of up that integers and maximum have in common: it goes to the maximum alone.
 __device__ __forceinline__ float q8_activation(const q8_i32x16_t& g, const q8_i32x16_t& u, float xs,
                                                const float (&gs)[4][4], const float (&us)[4][4], uint2 (&out)[4]) {
-    float a[16];
-    uint32_t mx = 0u;
+    float a[16], m = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-        const float gv = (float)g[v] * (xs * gs[v / 4][v % 4]), uv = (float)u[v] * (xs * us[v / 4][v % 4]);
-        a[v] = gv * fast_sigmoid(gv) * uv;
-        const uint32_t b = __float_as_uint(a[v]) & 0x7fffffffu;   // ordered as the numbers are, a NaN above them all
-        mx = b > mx ? b : mx;
+        const float gv = (float)g[v] * xs * gs[v / 4][v % 4], uv = (float)u[v] * us[v / 4][v % 4];
+        a[v] = gv * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-gv)) * uv;
+        m = __builtin_elementwise_maximum(m, fabsf(a[v]));   // a NaN stays
     }
-    const uint32_t o = (uint32_t)__shfl_xor((int)mx, 32, 64);
-    mx = o > mx ? o : mx;
-    const float m = __uint_as_float(mx), inv = mx < kQ8TinyBits ? 0.f : 32767.f * __builtin_amdgcn_rcpf(m);
+    m = __builtin_elementwise_maximum(m, __shfl_xor(m, 32, 64));
+    const float inv = m < kQ8Tiny ? 0.f : __builtin_amdgcn_rcpf(m);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < 4; ++q) {   // to the nearest of 32767 steps to one, in one instruction for two
         uint32_t w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            w[i] = ((uint32_t)q8_round16(a[4 * q + 2 * i], inv) & 0xffffu) |
-                   ((uint32_t)q8_round16(a[4 * q + 2 * i + 1], inv) << 16);
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_i16(a[4 * q + 2 * i] * inv, a[4 * q + 2 * i + 1] * inv));
         out[q] = make_uint2(w[0], w[1]);
     }
-    return m;
+    return m * fabsf(xs);
 }
+constexpr float kLog2e = 1.44269504088896341f;
 
 // eight bf16 from col on (of N) at an address that is aligned to one
 struct __attribute__((packed, aligned(2))) Q8B8 {
@@ -158,7 +143,7 @@ struct Q8Args {
     const int32_t *off, *map;
     const int8_t *w0, *w1;      // [E, N, pitch]; w1: up
     const float *s0, *s1;       // [E, N]
-    int pitch, N;
+    int pitch, N, tile_rows;    // tile_rows: the tile map's
     int16_t* a16;               // gate/up: [rows][a_pitch]
     float* gmax;                // [rows][a_pitch / 32]
     int a_pitch;
@@ -178,162 +163,229 @@ struct Q8Tile {
         e = a.map[4 + 2 * tile];
         row0 = a.map[4 + 2 * tile + 1];
         rows = a.off[e + 1] - row0;
+        rows = rows < a.tile_rows ? rows : a.tile_rows;
         return true;
     }
 };
 
-// =========================================================================================================
-// Many rows: 256 x 256 tiles (gate/up: the same 128 columns of both), 8 waves (2 x 4) of 128 x 64 each, one block per CU.
-// Units A(0) B(0) A(1) B(1) .. of 256 rows x 128 k run through five slots of 32 KiB, two to three of them on their way.
-// =========================================================================================================
-constexpr int kBigUnit = 256 * 128, kBigLds = 5 * kBigUnit;
+long q8_blocks(int N, int cols, int max_tiles) { return ((long)max_tiles * ((N + cols - 1) / cols) + 7) / 8 * 8; }
 
-template <bool DUAL>
-__device__ __forceinline__ int big_col(int ni) {
-    const int wn = (threadIdx.x >> 6) & 3;
-    return DUAL ? ni * 128 + wn * 32 : wn * 64 + ni * 32;
+// =========================================================================================================
+// Tiles of MT x MT (gate/up: the same MT / 2 columns of both).  Units A(0) B(0) A(1) B(1) .. of MT rows x 128 k run through
+// five slots, two to three of them on their way.
+//   256: 8 waves (2 x 4) of 128 x 64 each, 160 KiB, one block per CU: the most products per byte of LDS
+//   128: 4 waves (2 x 2) of 64 x 64 each, 80 KiB, two blocks per CU: where the weights' bytes are the bound, or 256 rows few
+// =========================================================================================================
+template <int MT, int WAVES>
+struct Tile8 {
+    static constexpr int kWaves = WAVES, kThreads = 64 * WAVES, kWn = WAVES / 2, kMi = MT / 64, kNi = MT / 32 / kWn,
+                         kLoads = MT / 8 / WAVES, kUnit = MT * 128, kLds = 5 * kUnit;
+    typedef q8_i32x16_t Acc[kMi][kNi];
+    __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    __device__ __forceinline__ static int wm() { return wave() / kWn; }
+    __device__ __forceinline__ static int wn() { return wave() % kWn; }
+    __device__ __forceinline__ static int first() { return wave() * 8 * kLoads; }   // row of the wave's share of a unit
+    // first column of the wave's ni-th 32 (DUAL: the first half of them of the first matrix), first row of its mi-th
+    template <bool DUAL>
+    __device__ __forceinline__ static int col(int ni) {
+        constexpr int H = kNi / 2;
+        return DUAL ? ni / H * (MT / 2) + wn() * 32 * H + ni % H * 32 : wn() * 32 * kNi + ni * 32;
+    }
+    __device__ __forceinline__ static int row(int mi) { return wm() * (MT / 2) + mi * 32; }
+};
+template <class W, bool DUAL, int MI>
+__device__ __forceinline__ void tile8_read(Q8Frags<MI, W::kNi>& f, const char* ua, const char* ub, int ks) {
+#pragma unroll
+    for (int ni = 0; ni < W::kNi; ++ni) f.b[ni] = q8_frag(ub, W::template col<DUAL>(ni), ks);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) f.a[mi] = q8_frag(ua, W::row(mi), ks);
 }
-template <bool DUAL>
-__device__ __forceinline__ void big_read(Q8Frags<4>& f, const char* ua, const char* ub, int ks) {
-    const int wm = threadIdx.x >> 8;
+template <int MI, int NI, int N>
+__device__ __forceinline__ void q8_mma(q8_i32x16_t (&acc)[N][NI], const Q8Frags<MI, NI>& f) {
 #pragma unroll
-    for (int ni = 0; ni < 2; ++ni) f.b[ni] = q8_frag(ub, big_col<DUAL>(ni), ks);
+    for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-    for (int mi = 0; mi < 4; ++mi) f.a[mi] = q8_frag(ua, wm * 128 + mi * 32, ks);
+        for (int ni = 0; ni < NI; ++ni)
+            acc[mi][ni] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.b[ni], f.a[mi], acc[mi][ni], 0, 0, 0);
 }
 // One pass: the four steps on A(p) = ua, B(p) = ub.  On entry both have landed, every wave has left the units of pass p - 1
 // (fill1, fill2), and f1 holds that pass's last step.  The slots are distinct, and saying so matters: an LDS read that may
 // observe a direct-to-LDS load in flight makes the compiler wait for all of them.
-template <bool DUAL>
-__device__ __forceinline__ void big_pass(q8_i32x16_t (&acc)[4][2], Q8Frags<4>& f0, Q8Frags<4>& f1, Q8Rows<4>& a,
-                                         Q8Rows<4>& b, bool more_a, bool more_b, char* __restrict__ fill1,
-                                         char* __restrict__ fill2, const char* __restrict__ ua,
-                                         const char* __restrict__ ub) {
-    const int first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32;
-    b.issue(fill1, first, more_b);       // B(p+1)
+template <class W, bool DUAL, int MI>
+__device__ __forceinline__ void tile8_pass(typename W::Acc& acc, Q8Frags<MI, W::kNi>& f0, Q8Frags<MI, W::kNi>& f1,
+                                           Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, bool more_a, bool more_b,
+                                           char* __restrict__ fill1, char* __restrict__ fill2,
+                                           const char* __restrict__ ua, const char* __restrict__ ub) {
+    b.issue(fill1, W::first(), more_b);  // B(p+1)
     __builtin_amdgcn_sched_barrier(0);   // the requests stay where they stand: sunk to the end of the pass they are late
-    big_read<DUAL>(f0, ua, ub, 0);
-    q8_mma<4>(acc, f1);
-    big_read<DUAL>(f1, ua, ub, 1);
-    q8_mma<4>(acc, f0);
+    tile8_read<W, DUAL, MI>(f0, ua, ub, 0);
+    q8_mma(acc, f1);
+    tile8_read<W, DUAL, MI>(f1, ua, ub, 1);
+    q8_mma(acc, f0);
     __builtin_amdgcn_sched_barrier(0);
-    a.issue(fill2, first, more_a);       // A(p+2)
+    a.issue(fill2, W::first(), more_a);  // A(p+2)
     __builtin_amdgcn_sched_barrier(0);
-    big_read<DUAL>(f0, ua, ub, 2);
-    q8_mma<4>(acc, f1);
-    big_read<DUAL>(f1, ua, ub, 3);
-    q8_mma<4>(acc, f0);
+    tile8_read<W, DUAL, MI>(f0, ua, ub, 2);
+    q8_mma(acc, f1);
+    tile8_read<W, DUAL, MI>(f1, ua, ub, 3);
+    q8_mma(acc, f0);
 }
-template <bool DUAL>
-__device__ __forceinline__ void big_mainloop(q8_i32x16_t (&acc)[4][2], Q8Rows<4>& a, Q8Rows<4>& b, int np, char* smem) {
-    const int first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32;
+// MI: the wave's 32-row blocks that hold rows (0: it only takes part in the loads)
+template <class W, bool DUAL, int MI>
+__device__ __forceinline__ void tile8_loop(typename W::Acc& acc, Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, int np, char* smem) {
+    constexpr int kUnit = W::kUnit, M = MI > 0 ? MI : 1;
     const q8_i32x4_t z = {0, 0, 0, 0};
-    Q8Frags<4> f0, f1;
+    Q8Frags<M, W::kNi> f0, f1;
 #pragma unroll
-    for (int mi = 0; mi < 4; ++mi) {
-        f1.a[mi] = z;
-        f1.b[mi & 1] = z;
+    for (int mi = 0; mi < M; ++mi) f1.a[mi] = z;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[mi][0][v] = acc[mi][1][v] = 0;
-    }
-    a.issue(smem, first, np > 1);
-    b.issue(smem + kBigUnit, first, np > 1);
-    a.issue(smem + 2 * kBigUnit, first, np > 2);
-    // at the top of pass p everything up to B(p) has landed for every thread, A(p+1) may be on its way
-    q8_wait_and_barrier<4>();
+    for (int ni = 0; ni < W::kNi; ++ni) f1.b[ni] = z;
     int sa = 0;   // slot of A(p) = 2p % 5
     for (int p = 0; p < np; ++p) {
         const int sb = sa + 1 < 5 ? sa + 1 : sa - 4, s3 = sa + 3 < 5 ? sa + 3 : sa - 2, s4 = sa + 4 < 5 ? sa + 4 : sa - 1;
-        big_pass<DUAL>(acc, f0, f1, a, b, p + 3 < np, p + 2 < np, smem + s3 * kBigUnit, smem + s4 * kBigUnit,
-                       smem + sa * kBigUnit, smem + sb * kBigUnit);
-        q8_wait_and_barrier<4>();
+        if (MI > 0) {
+            tile8_pass<W, DUAL, M>(acc, f0, f1, a, b, p + 3 < np, p + 2 < np, smem + s3 * kUnit, smem + s4 * kUnit,
+                                   smem + sa * kUnit, smem + sb * kUnit);
+        } else {
+            b.issue(smem + s3 * kUnit, W::first(), p + 2 < np);
+            a.issue(smem + s4 * kUnit, W::first(), p + 3 < np);
+        }
+        q8_wait_and_barrier<W::kLoads>();
         sa = sa + 2 < 5 ? sa + 2 : sa - 3;
     }
-    q8_mma<4>(acc, f1);
+    if (MI > 0) q8_mma(acc, f1);
+}
+// rows: valid ones of the tile, which may exceed it
+template <class W, bool DUAL>
+__device__ __forceinline__ void tile8_product(typename W::Acc& acc, Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, int np, int rows,
+                                              char* smem) {
+    constexpr int kUnit = W::kUnit;
+#pragma unroll
+    for (int mi = 0; mi < W::kMi; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < W::kNi; ++ni)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0;
+    a.issue(smem, W::first(), np > 1);
+    b.issue(smem + kUnit, W::first(), np > 1);
+    a.issue(smem + 2 * kUnit, W::first(), np > 2);
+    // at the top of pass p everything up to B(p) has landed for every thread, A(p+1) may be on its way
+    q8_wait_and_barrier<W::kLoads>();
+    const int left = rows - W::row(0);
+    if (left <= 0)
+        tile8_loop<W, DUAL, 0>(acc, a, b, np, smem);
+    else if (W::kMi == 2 && left <= 32)
+        tile8_loop<W, DUAL, 1>(acc, a, b, np, smem);
+    else
+        tile8_loop<W, DUAL, W::kMi>(acc, a, b, np, smem);
     q8_wait_and_barrier<0>();   // nothing may land in this LDS any more: it becomes the results'
 }
 
-__global__ __launch_bounds__(512) void q8_gateup_kernel(Q8Args g) {
-    __shared__ __align__(16) char smem[kBigLds];
+template <int MT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void q8_gateup_kernel(Q8Args g) {
+    typedef Tile8<MT, WAVES> W;
+    constexpr int H = W::kNi / 2, kCols = MT / 2, kPieces = kCols / 8;   // columns, 16-byte pieces of a row of results
+    __shared__ __align__(16) char smem[W::kLds];
     Q8Tile t;
-    if (!t.place(g, 128)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 2, wn = wave & 3;
-    Q8Rows<4> a, b;
-    a.init(g.x, g.pitch, wave * 32, [&](int r) {
+    if (!t.place(g, kCols)) return;
+    const int lane = threadIdx.x & 63;
+    Q8Rows<W::kLoads> a, b;
+    a.init(g.x, g.pitch, W::first(), [&](int r) {
         r = t.row0 + (r < t.rows ? r : t.rows - 1);   // rows past the last one repeat it; what they give is not stored
         return g.row_index ? g.row_index[r] : r;
     });
-    b.init(wave < 4 ? g.w0 : g.w1, g.pitch, wave * 32, [&](int r) {
-        const int n = t.n0 + (r & 127);
+    b.init(W::wave() < WAVES / 2 ? g.w0 : g.w1, g.pitch, W::first(), [&](int r) {
+        const int n = t.n0 + (r & (kCols - 1));
         return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
     });
-    q8_i32x16_t acc[4][2];
-    big_mainloop<true>(acc, a, b, g.pitch / 128, smem);
-    float gs[4][4], us[4][4];
-    const int c0 = t.n0 + wn * 32 + 4 * (lane >> 5);
+    // the scales are fetched ahead of the loop
+    float xs[W::kMi], gs[H][4][4], us[H][4][4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        q8_scales(g.s0 + (size_t)t.e * g.N, c0 + 8 * q, g.N, gs[q]);
-        q8_scales(g.s1 + (size_t)t.e * g.N, c0 + 8 * q, g.N, us[q]);
+    for (int mi = 0; mi < W::kMi; ++mi) {
+        const int r = W::row(mi) + (lane & 31), row = t.row0 + (r < t.rows ? r : t.rows - 1);
+        xs[mi] = g.x_scale[g.row_index ? g.row_index[row] : row];
     }
-    // results: rows of 128 columns, 16-byte pieces XOR-ed with the row
 #pragma unroll
-    for (int mi = 0; mi < 4; ++mi) {
-        const int r = wm * 128 + mi * 32 + (lane & 31), row = t.row0 + (r < t.rows ? r : t.rows - 1);
-        const float xs = g.x_scale[g.row_index ? g.row_index[row] : row];
-        uint2 o[4];
-        const float m = q8_activation(acc[mi][0], acc[mi][1], xs, gs, us, o);
-        if (lane < 32 && r < t.rows) g.gmax[(size_t)row * (g.a_pitch / kQ8Group) + (t.n0 / kQ8Group + wn)] = m;
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<uint2*>(smem + r * 256 + (((wn * 4 + q) ^ (r & 15)) << 4) + 8 * (lane >> 5)) = o[q];
+        for (int q = 0; q < 4; ++q) {
+            const int c = t.n0 + W::template col<true>(h) + 4 * (lane >> 5) + 8 * q;
+            q8_scales(g.s0 + (size_t)t.e * g.N, c, g.N, gs[h][q]);
+            q8_scales(g.s1 + (size_t)t.e * g.N, c, g.N, us[h][q]);
+        }
+    typename W::Acc acc;
+    tile8_product<W, true>(acc, a, b, g.pitch / 128, t.rows, smem);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            gs[h][v / 4][v % 4] *= kLog2e;
+            us[h][v / 4][v % 4] *= 1.0f / kLog2e;
+        }
+    // results: rows of kCols columns, 16-byte pieces XOR-ed with the row
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const int c0 = W::template col<true>(h);
+#pragma unroll
+        for (int mi = 0; mi < W::kMi; ++mi) {
+            const int r = W::row(mi) + (lane & 31);
+            uint2 o[4];
+            const float m = q8_activation(acc[mi][h], acc[mi][H + h], xs[mi], gs[h], us[h], o);
+            if (lane < 32 && r < t.rows) g.gmax[(size_t)(t.row0 + r) * (g.a_pitch / kQ8Group) + (t.n0 + c0) / kQ8Group] = m;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint2*>(smem + r * (2 * kCols) + (((c0 / 8 + q) ^ (r & (kPieces - 1))) << 4) + 8 * (lane >> 5)) =
+                    o[q];
+        }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = i * 32 + (threadIdx.x >> 4), c = threadIdx.x & 15;
-        const uint4 v = *reinterpret_cast<const uint4*>(smem + r * 256 + ((c ^ (r & 15)) << 4));
+    for (int i = 0; i < MT * kPieces / W::kThreads; ++i) {
+        const int r = i * (W::kThreads / kPieces) + threadIdx.x / kPieces, c = threadIdx.x % kPieces;
+        const uint4 v = *reinterpret_cast<const uint4*>(smem + r * (2 * kCols) + ((c ^ (r & (kPieces - 1))) << 4));
         if (r < t.rows) *reinterpret_cast<uint4*>(g.a16 + (size_t)(t.row0 + r) * g.a_pitch + t.n0 + 8 * c) = v;
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(512) void q8_down_kernel(Q8Args g) {
-    __shared__ __align__(16) char smem[kBigLds];
+template <int MT, int WAVES, typename T>
+__global__ __launch_bounds__(64 * WAVES, 2) void q8_down_kernel(Q8Args g) {
+    typedef Tile8<MT, WAVES> W;
+    constexpr int kPieces = MT / 8;
+    __shared__ __align__(16) char smem[W::kLds];
     Q8Tile t;
-    if (!t.place(g, 256)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 2, wn = wave & 3;
-    Q8Rows<4> a, b;
-    a.init(g.x, g.pitch, wave * 32, [&](int r) { return t.row0 + (r < t.rows ? r : t.rows - 1); });
-    b.init(g.w0, g.pitch, wave * 32, [&](int r) {
+    if (!t.place(g, MT)) return;
+    const int lane = threadIdx.x & 63;
+    Q8Rows<W::kLoads> a, b;
+    a.init(g.x, g.pitch, W::first(), [&](int r) { return t.row0 + (r < t.rows ? r : t.rows - 1); });
+    b.init(g.w0, g.pitch, W::first(), [&](int r) {
         const int n = t.n0 + r;
         return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
     });
-    q8_i32x16_t acc[4][2];
-    big_mainloop<false>(acc, a, b, g.pitch / 128, smem);
-    float as[4];
+    float as[W::kMi];   // fetched ahead of the loop
 #pragma unroll
-    for (int mi = 0; mi < 4; ++mi) {
-        const int r = wm * 128 + mi * 32 + (lane & 31);
+    for (int mi = 0; mi < W::kMi; ++mi) {
+        const int r = W::row(mi) + (lane & 31);
         as[mi] = g.x_scale[t.row0 + (r < t.rows ? r : t.rows - 1)];
     }
+    typename W::Acc acc;
+    tile8_product<W, false>(acc, a, b, g.pitch / 128, t.rows, smem);
 #pragma unroll
-    for (int ni = 0; ni < 2; ++ni)
+    for (int ni = 0; ni < W::kNi; ++ni)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int col = wn * 64 + ni * 32 + 8 * q + 4 * (lane >> 5);
+            const int col = W::template col<false>(ni) + 8 * q + 4 * (lane >> 5);
             float s[4];
             q8_scales(g.s0 + (size_t)t.e * g.N, t.n0 + col, g.N, s);
 #pragma unroll
-            for (int mi = 0; mi < 4; ++mi) {
-                const int r = wm * 128 + mi * 32 + (lane & 31);
+            for (int mi = 0; mi < W::kMi; ++mi) {
+                const int r = W::row(mi) + (lane & 31);
                 float o[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[i] = (float)acc[mi][ni][4 * q + i] * (as[mi] * s[i]);
                 if (sizeof(T) == 4) {
                     if (r < t.rows) q8_store4((float*)g.y + (size_t)(t.row0 + r) * g.N, t.n0 + col, g.N, o);
-                } else {   // rows of 256 columns, 16-byte pieces XOR-ed with the row
-                    *reinterpret_cast<uint2*>(smem + r * 512 + (((wn * 8 + ni * 4 + q) ^ (r & 31)) << 4) + 8 * (lane >> 5)) =
+                } else {   // rows of MT columns, 16-byte pieces XOR-ed with the row
+                    *reinterpret_cast<uint2*>(smem + r * (2 * MT) + (((col >> 3) ^ (r & (kPieces - 1))) << 4) + 8 * (lane >> 5)) =
                         make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
                 }
             }
@@ -341,11 +393,162 @@ __global__ __launch_bounds__(512) void q8_down_kernel(Q8Args g) {
     if (sizeof(T) == 4) return;
     __syncthreads();
 #pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int r = i * 16 + (threadIdx.x >> 5), c = threadIdx.x & 31;
-        const uint4 v = *reinterpret_cast<const uint4*>(smem + r * 512 + ((c ^ (r & 31)) << 4));
+    for (int i = 0; i < MT * kPieces / W::kThreads; ++i) {
+        const int r = i * (W::kThreads / kPieces) + threadIdx.x / kPieces, c = threadIdx.x % kPieces;
+        const uint4 v = *reinterpret_cast<const uint4*>(smem + r * (2 * MT) + ((c ^ (r & (kPieces - 1))) << 4));
         if (r < t.rows) q8_store8((bf16_t*)g.y + (size_t)(t.row0 + r) * g.N, t.n0 + 8 * c, g.N, v);
     }
+}
+
+template <int MT, int WAVES>
+int launch_q8_gateup(const Q8Args& a, int max_tiles, hipStream_t s) {
+    const long blocks = q8_blocks(a.N, MT / 2, max_tiles);
+    XMOE_LAUNCH(K_Q8_GATEUP, s,
+                hipLaunchKernelGGL((q8_gateup_kernel<MT, WAVES>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, s, a));
+    return XMOE_OK;
+}
+template <int MT, int WAVES>
+int launch_q8_down(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
+    const dim3 grid((unsigned)q8_blocks(a.N, MT, max_tiles)), block(64 * WAVES);
+    if (dt == XMOE_F32)
+        XMOE_LAUNCH(K_Q8_DOWN, s, hipLaunchKernelGGL((q8_down_kernel<MT, WAVES, float>), grid, block, 0, s, a));
+    else
+        XMOE_LAUNCH(K_Q8_DOWN, s, hipLaunchKernelGGL((q8_down_kernel<MT, WAVES, bf16_t>), grid, block, 0, s, a));
+    return XMOE_OK;
+}
+
+// =========================================================================================================
+// Gate and up of few rows (a decoding step): the weights' bytes are the bound.  32 rows and 64 columns of either matrix per
+// block of 4 waves, two blocks per CU.  A stage is 256 k, two cache lines of each row (one line of each costs memory a
+// tenth of its rate); two stages of 40 KiB, the second on its way while the first is multiplied.  Waves 0, 1 and 2, 3 take
+// half of a stage's k each, and their sums, which are integers, are added in LDS.  (Straight from memory to registers, 32
+// bytes of 32 rows at a time: slower by a quarter, the loads' addresses take the L1 cache too long.)
+// =========================================================================================================
+constexpr int kFewW = 128 * 256, kFewX = 32 * 256, kFewStage = kFewW + kFewX;
+__device__ __align__(16) const uint32_t kQ8Zero[4] = {0u, 0u, 0u, 0u};
+
+// A lane's pieces of the wave's share of an operand's stage ([rows][256 bytes]), 4 rows per load, piece (lane % 16) XOR-ed with
+// row % 16; those behind the end of K in the last stage come from a block of zeros
+template <int LOADS>
+struct Few8Rows {
+    const int8_t* p[LOADS];
+    uint32_t upper;   // bit i: the i-th piece lies in the stage's second half
+    template <class Source>
+    __device__ __forceinline__ void init(const int8_t* base, size_t pitch, int first, Source source) {
+        const int lane = threadIdx.x & 63;
+        upper = 0u;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = first + i * 4 + (lane >> 4), c = (lane & 15) ^ (r & 15);
+            p[i] = base + (size_t)source(r) * pitch + (c << 4);
+            upper |= (uint32_t)(c >> 3) << i;
+        }
+    }
+    __device__ __forceinline__ void issue(char* __restrict__ unit, int first, bool half) {   // half: K ends in the middle
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const bool out = half && ((upper >> i) & 1u);
+            q8_load16(out ? reinterpret_cast<const int8_t*>(kQ8Zero) : p[i], unit + (first + i * 4) * 256);
+            p[i] += 256;
+        }
+    }
+};
+__device__ __forceinline__ q8_i32x4_t few8_frag(const char* unit, int base, int ks) {
+    const int lane = threadIdx.x & 63, r = base + (lane & 31), c = 2 * ks + (lane >> 5);
+    return *reinterpret_cast<const q8_i32x4_t*>(unit + r * 256 + ((c ^ (r & 15)) << 4));
+}
+__device__ __forceinline__ void few8_stage(q8_i32x16_t (&acc)[2], Few8Rows<8>& w, Few8Rows<2>& x, bool more, bool half,
+                                           char* __restrict__ next, const char* __restrict__ cur) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = wave & 1, wk = wave >> 1;
+    if (more) {
+        w.issue(next, wave * 32, half);
+        x.issue(next + kFewW, wave * 8, half);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int ks = 4 * wk + i;
+        const q8_i32x4_t a = few8_frag(cur + kFewW, 0, ks);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+            acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(few8_frag(cur, 64 * n + 32 * wn, ks), a,
+                                                           acc[n], 0, 0, 0);
+    }
+}
+// The sums of the block's rows and columns; of all waves, 0 and 1 have them.
+__device__ __forceinline__ void few8_product(q8_i32x16_t (&acc)[2], Few8Rows<8>& w, Few8Rows<2>& x, int pitch, char* smem) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int stages = (pitch + 255) / 256;
+    const bool tail = pitch % 256 != 0;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[n][v] = 0;
+    w.issue(smem, wave * 32, tail && stages == 1);
+    x.issue(smem + kFewW, wave * 8, tail && stages == 1);
+    for (int s = 0; s < stages; ++s) {
+        q8_wait_and_barrier<0>();   // stage s has landed for every thread, and every wave is done with stage s - 1
+        char* cur = smem + (s & 1) * kFewStage;
+        few8_stage(acc, w, x, s + 1 < stages, tail && s + 2 == stages, smem + ((s + 1) & 1) * kFewStage, cur);
+    }
+    __syncthreads();
+    int* red = reinterpret_cast<int*>(smem) + (wave & 1) * 2048;
+    if (wave >= 2) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) red[(n * 16 + v) * 64 + lane] = acc[n][v];
+    }
+    __syncthreads();
+    if (wave < 2) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[n][v] += red[(n * 16 + v) * 64 + lane];
+    }
+}
+
+__global__ __launch_bounds__(256, 2) void q8_gateup_few_kernel(Q8Args g) {
+    __shared__ __align__(16) char smem[2 * kFewStage];
+    Q8Tile t;
+    if (!t.place(g, 64)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, r = lane & 31;
+    Few8Rows<8> w;
+    Few8Rows<2> x;
+    w.init(wave < 2 ? g.w0 : g.w1, g.pitch, wave * 32, [&](int c) {
+        const int n = t.n0 + (c & 63);
+        return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
+    });
+    x.init(g.x, g.pitch, wave * 8, [&](int i) {
+        i = t.row0 + (i < t.rows ? i : t.rows - 1);
+        return g.row_index ? g.row_index[i] : i;
+    });
+    const int row = t.row0 + (r < t.rows ? r : t.rows - 1), c0 = t.n0 + 32 * (wave & 1);
+    float xs = g.x_scale[g.row_index ? g.row_index[row] : row], gs[4][4], us[4][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        q8_scales(g.s0 + (size_t)t.e * g.N, c0 + 4 * half + 8 * q, g.N, gs[q]);
+        q8_scales(g.s1 + (size_t)t.e * g.N, c0 + 4 * half + 8 * q, g.N, us[q]);
+    }
+    q8_i32x16_t acc[2];
+    few8_product(acc, w, x, g.pitch, smem);
+    if (wave >= 2) return;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        gs[v / 4][v % 4] *= kLog2e;
+        us[v / 4][v % 4] *= 1.0f / kLog2e;
+    }
+    uint2 o[4];
+    const float m = q8_activation(acc[0], acc[1], xs, gs, us, o);
+    if (r >= t.rows) return;
+    if (half == 0) g.gmax[(size_t)row * (g.a_pitch / kQ8Group) + c0 / kQ8Group] = m;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(g.a16 + (size_t)row * g.a_pitch + c0 + 4 * half + 8 * q) = o[q];
+}
+
+int launch_q8_gateup_few(const Q8Args& a, int max_tiles, hipStream_t s) {
+    XMOE_LAUNCH(K_Q8_GATEUP_FEW, s, hipLaunchKernelGGL(q8_gateup_few_kernel, dim3((unsigned)q8_blocks(a.N, 64, max_tiles)),
+                                                       dim3(256), 0, s, a));
+    return XMOE_OK;
 }
 
 // =========================================================================================================
@@ -432,7 +635,15 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restri
     }
 }
 
-long q8_blocks(int N, int cols, int max_tiles) { return ((long)max_tiles * ((N + cols - 1) / cols) + 7) / 8 * 8; }
+
+// Rows of a tile, by the mean load.  Measured (MI355X, all launches together, us, 256 | 128 | 32 with 128-row down tiles):
+//     mean rows                           1 - 2         8          16         62        124       248       500       1000
+//     64 experts + 2, d 2048, f 1408    122|99|92   177|146|141    - |153|156  197|179   236|202   281|290   479|490   834|885
+//     8 experts, d 2048, f 1408              (4) - |44|43           - |44|42    62|44     70|50     75|60     84|92   239|237 (2048)
+//     256 experts, d 2048, f 512        - |185|171       -         - |218|205  292|244   346|322   497|485
+//     64 experts, d 2048, Zipf load                                            186|171 (96)  260|253 (192)  431|407 (384)
+//     32 experts + 1, d 4096, f 1024                                           206|184 (155)  245|262 (310)  406|426 (621)
+int q8_tile_rows(int B, int E) { return B <= 16ll * E ? 32 : B <= 256ll * E ? 128 : 256; }
 
 }  // namespace
 }  // namespace xmoe
@@ -473,7 +684,7 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
     const int fp = q8_pitch(f), dp = q8_pitch(d);
     char* p = (char*)ws;
     int32_t* map = (int32_t*)p;
-    p += ffn_tilemap_bytes(B, E);
+    p += ffn_q8_tilemap_bytes(B, E);
     int16_t* a16 = (int16_t*)p;
     p += align_up((size_t)B * fp * 2, 256);
     float* gmax = (float*)p;
@@ -482,27 +693,23 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
     p += align_up((size_t)B * fp, 256);
     float* as = (float*)p;
     hipStream_t s = (hipStream_t)stream;
-    const int tile_rows = 256, max_tiles = ffn_max_tiles(B, E, tile_rows);
-    const long up_blocks = q8_blocks(f, 128, max_tiles), down_blocks = q8_blocks(d, 256, max_tiles);
-    if ((up_blocks > down_blocks ? up_blocks : down_blocks) * 512 >= (1l << 32)) return XMOE_ERR_UNSUPPORTED;   // a grid's threads
-    int st = launch_tile_map(expert_offsets, E, tile_rows, max_tiles, map, map + ffn_sched_offset(B, E), false, s);
+    const int tile_rows = q8_tile_rows(B, E), max_tiles = ffn_max_tiles(B, E, tile_rows);
+    // a grid has fewer than 2^32 threads: tiles of 64 columns and 256 threads are the most
+    if (q8_blocks(f > d ? f : d, 64, max_tiles) * 256 >= (1l << 32)) return XMOE_ERR_UNSUPPORTED;
+    int st = launch_tile_map(expert_offsets, E, tile_rows, max_tiles, map, map + ffn_q8_sched_offset(B, E), false, s);
     if (st != XMOE_OK) return st;
     const Q8Args up = {(const int8_t*)xq, x_scale, row_index, expert_offsets, map, (const int8_t*)wgq, (const int8_t*)wuq,
-                       g_scale, u_scale, dp, f, a16, gmax, fp, nullptr};
-    const Q8Args down = {aq, as, nullptr, expert_offsets, map, (const int8_t*)wdq, nullptr, d_scale, nullptr, fp, d, nullptr,
-                         nullptr, 0, y};
-    XMOE_LAUNCH(K_Q8_GATEUP, s,
-                hipLaunchKernelGGL(q8_gateup_kernel, dim3((unsigned)up_blocks), dim3(512), 0, s, up));
+                       g_scale, u_scale, dp, f, tile_rows, a16, gmax, fp, nullptr};
+    const Q8Args down = {aq, as, nullptr, expert_offsets, map, (const int8_t*)wdq, nullptr, d_scale, nullptr, fp, d, tile_rows,
+                         nullptr, nullptr, 0, y};
+    st = tile_rows == 256 ? launch_q8_gateup<256, 8>(up, max_tiles, s)
+         : tile_rows == 128 ? launch_q8_gateup<128, 4>(up, max_tiles, s)
+                            : launch_q8_gateup_few(up, max_tiles, s);
+    if (st != XMOE_OK) return st;
     XMOE_LAUNCH(K_Q8_ROWS, s,
                 hipLaunchKernelGGL(q8_rows_kernel, dim3((unsigned)((B + 3) / 4)), dim3(256), 0, s, a16, gmax, expert_offsets,
                                    E, f, fp, aq, as));
-    if (dt == XMOE_F32)
-        XMOE_LAUNCH(K_Q8_DOWN, s,
-                    hipLaunchKernelGGL(q8_down_kernel<float>, dim3((unsigned)down_blocks), dim3(512), 0, s, down));
-    else
-        XMOE_LAUNCH(K_Q8_DOWN, s,
-                    hipLaunchKernelGGL(q8_down_kernel<bf16_t>, dim3((unsigned)down_blocks), dim3(512), 0, s, down));
-    return XMOE_OK;
+    return tile_rows == 256 ? launch_q8_down<256, 8>(down, max_tiles, dt, s) : launch_q8_down<128, 4>(down, max_tiles, dt, s);
 }
 
 }  // extern "C"

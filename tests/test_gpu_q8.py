@@ -10,16 +10,20 @@ import pytest
 import torch
 
 import oracle
+from gpu_util import launched
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 NEAR = 127 * (168 * U + 2.0 ** -16)
-ROWS = {
+ROWS = {      # mean loads up to 16, up to 256 and above: the three tile sizes
     "edges": [0, 1, 255, 256, 257, 0, 31],
-    "few": [1, 0, 2, 33, 0, 64, 65],
-    "one long": [0, 700, 3],
+    "few": [1, 0, 2, 33, 0, 64, 65] + [0] * 8,
+    "middle": [1, 0, 2, 33, 0, 64, 65],
+    "one long": [0, 900, 3],
+    "even": [300, 257, 290],
     "single": [1],
 }
+KERNELS = {"edges": 128, "few": 32, "middle": 128, "one long": 256, "even": 256, "single": 32}
 WIDTHS = [(1, 1), (64, 64), (130, 200), (257, 96), (1000, 712), (384, 1409)]   # d, f
 
 
@@ -52,10 +56,10 @@ def call(m, c, dt, B=None, fill=7.0):
     y = torch.full((B + 1, c["d"]), fill, dtype=dt, device="cuda")
     ws = m.alloc_workspace(m.xmoe_workspace_bytes(m.WS_FFN_Q8_FWD, B, c["d"], c["E"], 1, c["f"], m.dtype_code(dt)))
     ws.random_(0, 256)
-    m.xmoe_expert_ffn_q8_fwd(dev(padded(c["x"])), dev(c["xs"]), dev(c["off"]), dev(padded(c["w"][0])), dev(c["ws"][0]),
-                             dev(padded(c["w"][1])), dev(c["ws"][1]), dev(padded(c["w"][2])), dev(c["ws"][2]), y[:B], ws,
-                             row_index=dev(c["index"]))
-    torch.cuda.synchronize()
+    args = [dev(a) for a in (padded(c["x"]), c["xs"], c["off"], padded(c["w"][0]), c["ws"][0], padded(c["w"][1]), c["ws"][1],
+                             padded(c["w"][2]), c["ws"][2])]
+    kernels = launched(m, lambda: m.xmoe_expert_ffn_q8_fwd(*args, y[:B], ws, row_index=dev(c["index"])))
+    assert kernels >= {"q8_gateup_few_kernel" if B <= 16 * c["E"] else "q8_gateup_kernel", "q8_down_kernel"}, kernels
     assert bool((y[B] == fill).all())
     return y[:B].cpu()
 
@@ -82,6 +86,7 @@ def check(c, got, dt):
 def test_against_the_oracle(rows, d, f, gathered, dt):
     import paper_2508_13337_amd as m
     c = make(ROWS[rows], d, f, gathered)
+    assert (32 if c["B"] <= 16 * c["E"] else 128 if c["B"] <= 256 * c["E"] else 256) == KERNELS[rows]
     check(c, call(m, c, dt), dt)
 
 
