@@ -34,117 +34,83 @@ struct LayerArgs {
 };
 
 // ---------------------------------------------------------------------------------------------------------
-// route: one block of 8 waves per token.  Wave w takes the experts 8 w .., 8 (w + 8) ..; lane l is the partial sum l.
-// The router's rows are contiguous, and a lane wants 16 bytes of a row of its own: a stage of whole rows goes through LDS (rows
-// 16 bytes further apart than in memory, which keeps the lanes off each other's banks), the next one is on its way in
-// registers.  Straight from memory every wave would touch every line of the router.
+// route: one block of 8 waves per token.  64 rows of the router are contiguous, and a thread takes 16 bytes of them (EV
+// experts of one row: one of the 64 partial sums of each; EV = 1 where rows are no whole 16-byte pieces), those of the next 64
+// rows, and so on: whole lines, every load independent of every other.  The partial sums are folded in LDS, and the first
+// wave picks the experts.  Latency: a router of 256 KiB is on its way to one CU at once, in registers.
 // ---------------------------------------------------------------------------------------------------------
 // elements at an address that is aligned to one
 template <typename T, int N>
 struct __attribute__((packed, aligned(sizeof(T)))) LayerVec {
     T v[N];
 };
-constexpr int kRouteLds = 64 << 10, kRoutePieces = 8;   // of 16 bytes, per thread and stage: 512 * 8 of them are a stage's most
-constexpr int kRouteSteps = 32;                         // of 64 rows: a stage's most
+constexpr int kRouteExperts = 128, kRouteX = 4096;   // experts at most; values of x in LDS at a time
+constexpr int kRouteSteps = 16;                      // of 64 rows, whose loads are in flight together
 
-// pitch: bytes of a staged row, 0: rows that are no whole 16-byte pieces are read from memory
-template <typename T, int PER_LANE>
-__global__ __launch_bounds__(512) void layer_route_kernel(LayerArgs g, int pitch, int steps) {
-    __shared__ __align__(16) char stage[kRouteLds];
-    __shared__ float row[XMOE_MAX_EXPERTS], xs[64 * kRouteSteps];
+template <typename T, int EV>
+__global__ __launch_bounds__(512) void layer_route_kernel(LayerArgs g) {
+    __shared__ float xs[kRouteX], part[64 * kRouteExperts];   // part: [partial sum][expert]
     const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const T* x = (const T*)g.x + (size_t)t * g.d;
     const T* w = (const T*)g.w_router;
-    float p[PER_LANE][8];
+    const int per_row = g.E / EV, chunk = 64 * per_row;   // pieces of a row, of 64 rows
+    // every thread has the same number of pieces but for the last round
+    for (int n0 = 0; n0 < chunk; n0 += 512) {
+        const int n = n0 + threadIdx.x < chunk ? n0 + threadIdx.x : chunk - 1, l = n / per_row;   // past the last: not stored
+        float p[EV];
 #pragma unroll
-    for (int h = 0; h < PER_LANE; ++h)
+        for (int j = 0; j < EV; ++j) p[j] = 0.f;
+        for (int i0 = 0; i0 < g.d; i0 += kRouteX) {
+            const int len = g.d - i0 < kRouteX ? g.d - i0 : kRouteX;
+            const T* src = w + (size_t)i0 * g.E + (size_t)n * EV;
+            LayerVec<T, EV> q[kRouteSteps];
+            auto fetch = [&](int m) {   // rows i0 + 64 m + l ..; one past the end: row 64 m0 + l of the chunk again, not used
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[h][j] = 0.f;
-    if (pitch) {
-        const int per_row = pitch / 16 - 1, stage_rows = 64 * steps;
-        const uint4* src = reinterpret_cast<const uint4*>(w);
-        int at[kRoutePieces];   // LDS addresses of the thread's pieces
-        uint4 v[kRoutePieces];
-        T xv[kRouteSteps / 8];
-#pragma unroll
-        for (int u = 0; u < kRoutePieces; ++u) {
-            const int n = threadIdx.x + 512 * u, r = n / per_row;
-            at[u] = r < stage_rows ? r * pitch + (n - r * per_row) * 16 : -1;
-        }
-        auto fetch = [&](int row0) {
-            const int n_valid = (g.d - row0) * per_row;   // pieces left
-#pragma unroll
-            for (int u = 0; u < kRoutePieces; ++u) {
-                const int n = threadIdx.x + 512 * u;
-                v[u] = at[u] >= 0 && n < n_valid ? src[(size_t)row0 * per_row + n] : make_uint4(0u, 0u, 0u, 0u);
-            }
-#pragma unroll
-            for (int u = 0; u < kRouteSteps / 8; ++u) {
-                const int n = row0 + threadIdx.x + 512 * u;
-                xv[u] = x[n < g.d ? n : g.d - 1];
-            }
-        };
-        fetch(0);
-        for (int row0 = 0; row0 < g.d; row0 += stage_rows) {
-            __syncthreads();   // the last stage has been read
-#pragma unroll
-            for (int u = 0; u < kRoutePieces; ++u)
-                if (at[u] >= 0) *reinterpret_cast<uint4*>(stage + at[u]) = v[u];
-#pragma unroll
-            for (int u = 0; u < kRouteSteps / 8; ++u) xs[threadIdx.x + 512 * u] = to_float(xv[u]);
+                for (int u = 0; u < kRouteSteps; ++u)
+                    q[u] = *reinterpret_cast<const LayerVec<T, EV>*>(src + (size_t)(64 * (m + u) + l < len ? m + u : 0) * chunk * EV);
+            };
+            // the row l itself may be past the end of a short router: its first piece stands in
+            if (l >= len) src = w;
+            fetch(0);
+            if (n0 > 0 || i0 > 0) __syncthreads();
+            for (int i = threadIdx.x; i < len; i += 512) xs[i] = to_float(x[i0 + i]);
             __syncthreads();
-            if (row0 + stage_rows < g.d) fetch(row0 + stage_rows);
-            for (int s = 0; s < steps; ++s) {
-                const int i = row0 + 64 * s + lane;
-                if (i >= g.d) break;
-                const float a = xs[64 * s + lane];
-                const char* r = stage + (64 * s + lane) * pitch;
+            for (int m = 0; 64 * m < len; m += kRouteSteps) {
 #pragma unroll
-                for (int h = 0; h < PER_LANE; ++h) {
-                    const int e0 = 8 * wave + 64 * h;
-                    if (e0 < g.E) {
-                        const LayerVec<T, 8> q = *reinterpret_cast<const LayerVec<T, 8>*>(r + e0 * (int)sizeof(T));
+                for (int u = 0; u < kRouteSteps; ++u) {
+                    const int i = 64 * (m + u) + l;
+                    if (i < len) {
+                        const float a = xs[i];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) p[h][j] = fmaf(a, to_float(q.v[j]), p[h][j]);
+                        for (int j = 0; j < EV; ++j) p[j] = fmaf(a, to_float(q[u].v[j]), p[j]);
                     }
                 }
+                if (64 * (m + kRouteSteps) < len) fetch(m + kRouteSteps);
             }
         }
-    } else {
-        for (int i = lane; i < g.d; i += 64) {
-            const float a = to_float(x[i]);
+        if (n0 + (int)threadIdx.x < chunk) {
 #pragma unroll
-            for (int h = 0; h < PER_LANE; ++h)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int e = 8 * wave + 64 * h + j;
-                    if (e < g.E) p[h][j] = fmaf(a, to_float(w[(size_t)i * g.E + e]), p[h][j]);
-                }
+            for (int j = 0; j < EV; ++j) part[n * EV + j] = p[j];   // [l][expert]: the pieces' own order
         }
     }
-#pragma unroll
-    for (int h = 0; h < PER_LANE; ++h) {
-        const int e0 = 8 * wave + 64 * h;
-        if (e0 >= g.E) break;
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[h][j] += __shfl_xor(p[h][j], off, 64);
-        if (lane == 0) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (e0 + j < g.E) {
-                    const float l = g.bias ? p[h][j] + g.bias[e0 + j] : p[h][j];
-                    row[e0 + j] = l;
-                    g.logits[(size_t)t * g.E + e0 + j] = l;
-                }
-        }
+    __syncthreads();
+    for (int off = 32; off >= 1; off /= 2) {
+        for (int i = threadIdx.x; i < off * g.E; i += 512) part[i] += part[i + off * g.E];
+        __syncthreads();
+    }
+    for (int e = threadIdx.x; e < g.E; e += 512) {
+        const float v = g.bias ? part[e] + g.bias[e] : part[e];
+        g.logits[(size_t)t * g.E + e] = v;
+        xs[e] = v;
     }
     __syncthreads();
     if (wave > 0) return;
     int idx;
     float wt;
-    route_token<PER_LANE>(row, g.E, g.k, idx, wt);
+    if (g.E <= 64)
+        route_token<1>(xs, g.E, g.k, idx, wt);
+    else
+        route_token<kRouteExperts / 64>(xs, g.E, g.k, idx, wt);
     if (lane < g.k) {
         g.topk_idx[(size_t)t * g.k + lane] = idx;
         g.topk_w[(size_t)t * g.k + lane] = wt;
@@ -621,20 +587,11 @@ int launch_alu(const LayerArgs& a, int active, hipStream_t s) {
 
 template <typename T>
 int launch_layer_route(const LayerArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)a.T);
-    const int row_bytes = a.E * (int)sizeof(T);
-    int pitch = row_bytes + 16;
-    // rows of a stage: what LDS and 512 * kRoutePieces pieces hold, in steps of 64.  An expert's eight are whole pieces too.
-    int steps = kRouteLds / (64 * pitch) < kRouteSteps ? kRouteLds / (64 * pitch) : kRouteSteps;
-    while (steps > 1 && steps * 64 * (row_bytes / 16) > 512 * kRoutePieces) --steps;
-    if (a.E % 8 || !aligned16(a.w_router) || steps < 1 || steps * 64 * (row_bytes / 16) > 512 * kRoutePieces) pitch = 0;
-#define XMOE_CALL(PL) \
-    XMOE_LAUNCH(K_LAYER_ROUTE, s, hipLaunchKernelGGL((layer_route_kernel<T, PL>), grid, dim3(512), 0, s, a, pitch, steps))
-    if (a.E <= 64) XMOE_CALL(1);
-    else if (a.E <= 128) XMOE_CALL(2);
-    else if (a.E <= 256) XMOE_CALL(4);
-    else XMOE_CALL(8);
-#undef XMOE_CALL
+    constexpr int EV = 16 / (int)sizeof(T);
+    if (a.E % EV == 0 && aligned16(a.w_router))
+        XMOE_LAUNCH(K_LAYER_ROUTE, s, hipLaunchKernelGGL((layer_route_kernel<T, EV>), dim3((unsigned)a.T), dim3(512), 0, s, a));
+    else
+        XMOE_LAUNCH(K_LAYER_ROUTE, s, hipLaunchKernelGGL((layer_route_kernel<T, 1>), dim3((unsigned)a.T), dim3(512), 0, s, a));
     return XMOE_OK;
 }
 
@@ -674,7 +631,7 @@ extern "C" int xmoe_layer_few_fwd(const void* x, const void* w_router, const flo
     p += align_up(rows * f * dtype_size(dt), 256);
     a.y = (float*)p;
     int st;
-    if ((size_t)d * E * dtype_size(dt) <= kRouteBytes) {
+    if (E <= kRouteExperts && (size_t)d * E * dtype_size(dt) <= kRouteBytes) {
         st = dt == XMOE_F32 ? launch_layer_route<float>(a, s) : launch_layer_route<bf16_t>(a, s);
     } else {
         st = xmoe_gate_logits(x, w_router, bias, logits, T, d, E, dt, stream);
