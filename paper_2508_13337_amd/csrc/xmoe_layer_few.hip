@@ -183,11 +183,11 @@ __device__ __forceinline__ int layer_tokens(LayerPlan& pl, int e) {
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// matrix cores (bf16, d % 64 == 0, f % 64 == 0, 16-byte aligned)
+// matrix cores (bf16, d % 8 == 0, f % 8 == 0, 16-byte aligned: rows are whole 16-byte pieces)
 // ---------------------------------------------------------------------------------------------------------
-// A block of 4 waves multiplies up to 32 rows with COLS columns, 32 k to a stage, on a ring of direct-to-LDS stages.
-// LDS of a stage: 32 k-rows of COLS columns, whose 16-byte pieces are XOR-ed with 4 * (k-row % 4), then 32 rows of x with 64
-// bytes each, pieces XOR-ed with (row / 4) % 4: the fragment reads fall on all banks.
+// A block of 4 waves multiplies up to 32 rows with COLS columns, KS k to a stage, on a ring of direct-to-LDS stages.
+// LDS of a stage: KS k-rows of COLS columns, whose 16-byte pieces are XOR-ed with 4 * (k-row % 4), then 32 rows of x with 2 KS
+// bytes each, pieces XOR-ed with (row / 4) % 4 or (row / 2) % 8: the fragment reads fall on all banks.
 // The plan lies behind the ring in the same array: LDS reads of an object of its own would make the compiler wait for every
 // direct-to-LDS load in flight at each of the ring's reads.
 typedef __attribute__((ext_vector_type(8))) __bf16 layer_bf16x8_t;
@@ -195,34 +195,41 @@ typedef __attribute__((ext_vector_type(16))) float layer_f32x16_t;
 typedef __attribute__((ext_vector_type(4))) short layer_s16x4_t;
 typedef __attribute__((ext_vector_type(8))) short layer_s16x8_t;
 
-constexpr int kRingK = 32;
+__device__ __align__(16) const uint32_t kRingZero[4] = {0u, 0u, 0u, 0u};
 __device__ __forceinline__ void ring_load16(const bf16_t* p, char* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
                                      (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 // DUAL: the columns are COLS / 2 of two matrices each
-template <int COLS, bool DUAL, int STAGES>
+template <int COLS, bool DUAL, int KS, int STAGES>
 struct Ring {
-    static constexpr int kW = kRingK * COLS * 2, kStage = kW + 32 * kRingK * 2, kBytes = STAGES * kStage;
-    static constexpr int kLoads = COLS / 64;       // of weights, per wave and stage; waves 0 and 1 fetch a half of x each
+    static constexpr int kW = KS * COLS * 2, kStage = kW + 32 * KS * 2, kBytes = STAGES * kStage;
+    static constexpr int kLoads = kW / 4096;       // of weights, per wave and stage
+    static constexpr int kPieces = KS / 8;         // of a row of x; with 64 k every wave fetches 8 rows, with 32 waves 0 and 1 16
+    static constexpr bool kAllX = KS == 64;
     static constexpr int kBlocks = COLS / 128;     // of 32 columns, per wave
     static constexpr int kRows = 1024 / (2 * COLS);   // k-rows of a load
     const bf16_t *w[kLoads], *x;   // of the stage issued next
     size_t step;                   // elements between the weights of two stages
     int left;                      // stages behind the one issued next
+    uint32_t out;                  // bit i: the i-th piece of weights (bit kLoads: of x) lies behind K in the last stage
 
-    // rows: source(r) is row r's element 0; w0, w1: element (first k, n0) of the matrices, N columns of which cols exist
+    __host__ __device__ static int stages(int K) { return (K + KS - 1) / KS; }
+    __device__ __forceinline__ static int x_piece(int r, int c) { return c ^ (kAllX ? (r >> 1) & 7 : (r >> 2) & 3); }
+    // rows: source(r) is row r's first element; w0, w1: element (first k, n0) of the matrices, N columns of which cols exist
     template <class Source>
-    __device__ __forceinline__ void init(Source source, int rows, const bf16_t* w0, const bf16_t* w1, int N, int cols,
-                                         int stages) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __device__ __forceinline__ void init(Source source, int rows, const bf16_t* w0, const bf16_t* w1, int N, int cols, int K) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = stages(K), tail = K - KS * (n - 1);
+        out = 0u;
         {
-            const int r = (wave & 1) * 16 + (lane >> 2), c = (lane & 3) ^ ((r >> 2) & 3);
+            const int r = (kAllX ? wave : wave & 1) * (64 / kPieces) + lane / kPieces, c = x_piece(r, lane % kPieces);
             x = source(r < rows ? r : rows - 1) + 8 * c;   // rows past the last one repeat it; what they give is not stored
+            if (8 * c >= tail) out |= 1u << kLoads;
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int kr = wave * 8 + i * kRows + lane * 8 / COLS;
+            const int kr = wave * (KS / 4) + i * kRows + lane * 8 / COLS;
+            if (kr >= tail) out |= 1u << i;
             int col = 8 * ((lane & (COLS / 8 - 1)) ^ ((kr & 3) << 2));
             const bf16_t* b = w0;
             if (DUAL && col >= COLS / 2) {
@@ -232,26 +239,33 @@ struct Ring {
             if (col >= cols) col = 0;   // past the edge: not stored
             w[i] = b + (size_t)kr * N + col;
         }
-        step = (size_t)kRingK * N;
-        left = stages - 1;
+        step = (size_t)KS * N;
+        left = n - 1;
     }
-    // behind the last stage that one is fetched again, so that the counts stay uniform
+    // pieces behind K come from a block of zeros; behind the last stage that one is fetched again, so that the counts stay
+    // uniform, and not used
     __device__ __forceinline__ void issue(char* __restrict__ stage) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const bool more = left > 0;
+        if (left == 0) {   // the last stage: from now on
+            const bf16_t* zero = reinterpret_cast<const bf16_t*>(kRingZero);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                if ((out >> i) & 1u) w[i] = zero;
+            if ((out >> kLoads) & 1u) x = zero;
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             ring_load16(w[i], stage + wave * (kW / 4) + i * 1024);
-            w[i] += more ? step : 0;
+            w[i] += left > 0 ? step : 0;
         }
-        if (wave < 2) ring_load16(x, stage + kW + wave * 1024);
-        x += more ? kRingK : 0;
+        if (kAllX || wave < 2) ring_load16(x, stage + kW + wave * 1024);
+        x += left > 0 ? KS : 0;
         --left;
     }
     // at most N stages of the wave's loads on their way, its LDS reads returned
     template <int N>
     __device__ __forceinline__ static void wait() {
-        if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 2)
+        if (kAllX || __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 2)
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N * (kLoads + 1)) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N * kLoads) : "memory");
@@ -276,7 +290,7 @@ struct Ring {
     }
     __device__ __forceinline__ static layer_bf16x8_t frag_x(const char* stage, int ks) {
         const int lane = threadIdx.x & 63, r = lane & 31, c = 2 * ks + (lane >> 5);
-        return *reinterpret_cast<const layer_bf16x8_t*>(stage + kW + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+        return *reinterpret_cast<const layer_bf16x8_t*>(stage + kW + r * (2 * KS) + (x_piece(r, c) << 4));
     }
     // Refills the stage read before the last barrier and multiplies `cur`.  The two are distinct, and saying so matters: an
     // LDS read that may observe a direct-to-LDS load in flight makes the compiler wait for all of them.
@@ -284,7 +298,7 @@ struct Ring {
                                             const char* __restrict__ cur) {
         issue(next);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < KS / 16; ++ks) {
             const layer_bf16x8_t a = frag_x(cur, ks);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -292,7 +306,7 @@ struct Ring {
         }
     }
     // acc[b], register v of lane l: row l % 32, column 8 (v/4) + 4 (l/32) + v%4 of the wave's b-th 32
-    __device__ __forceinline__ void run(layer_f32x16_t (&acc)[kBlocks], char* smem, int stages) {
+    __device__ __forceinline__ void run(layer_f32x16_t (&acc)[kBlocks], char* smem, int n) {
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -300,7 +314,7 @@ struct Ring {
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s) issue(smem + s * kStage);
         int cur = 0, next = STAGES - 1;
-        for (int i = 0; i < stages; ++i) {
+        for (int i = 0; i < n; ++i) {
             // stage i has landed for every thread, and every wave is done with stage i - 1, which is refilled now
             wait<STAGES - 2>();
             asm volatile("s_barrier" ::: "memory");
@@ -320,9 +334,9 @@ __device__ __forceinline__ void layer_store_act(const LayerArgs& g, int row, int
 }
 
 // COLS / 2 columns of A of one expert
-template <int COLS, int STAGES>
+template <int COLS, int KS, int STAGES>
 __global__ __launch_bounds__(256, 2) void layer_up_few_kernel(LayerArgs g) {
-    typedef Ring<COLS, true, STAGES> R;
+    typedef Ring<COLS, true, KS, STAGES> R;
     __shared__ __align__(16) char smem[R::kBytes + sizeof(LayerPlan)];
     LayerPlan& pl = *reinterpret_cast<LayerPlan*>(smem + R::kBytes);
     layer_plan(pl, g);
@@ -333,9 +347,9 @@ __global__ __launch_bounds__(256, 2) void layer_up_few_kernel(LayerArgs g) {
     const size_t we = (size_t)e * g.d * g.f + n0;
     R ring;
     ring.init([&](int r) { return (const bf16_t*)g.x + (size_t)pl.tok[r] * g.d; }, rows, (const bf16_t*)g.wg + we,
-              (const bf16_t*)g.wu + we, g.f, g.f - n0, g.d / kRingK);
+              (const bf16_t*)g.wu + we, g.f, g.f - n0, g.d);
     layer_f32x16_t acc[R::kBlocks];
-    ring.run(acc, smem, g.d / kRingK);
+    ring.run(acc, smem, R::stages(g.d));
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31;
     if (r >= rows) return;
     const int col = n0 + COLS / 8 * wave + 4 * (lane >> 5);
@@ -352,20 +366,21 @@ __global__ __launch_bounds__(256, 2) void layer_up_few_kernel(LayerArgs g) {
 }
 
 // 256 columns of an expert's output, over a slab of f
-constexpr int kDownCols = 256, kDownStages = 4;
+constexpr int kDownCols = 256, kDownK = 32, kDownStages = 4;
 __global__ __launch_bounds__(256, 2) void layer_down_few_kernel(LayerArgs g) {
-    typedef Ring<kDownCols, false, kDownStages> R;
+    typedef Ring<kDownCols, false, kDownK, kDownStages> R;
     __shared__ __align__(16) char smem[R::kBytes + sizeof(LayerPlan)];
     LayerPlan& pl = *reinterpret_cast<LayerPlan*>(smem + R::kBytes);
     layer_plan(pl, g);
     const int nt = (g.d + kDownCols - 1) / kDownCols, per = nt * g.slabs, i = blockIdx.x / per;
     if (i >= pl.n) return;
     const int slab = (blockIdx.x - i * per) / nt, n0 = (blockIdx.x - i * per - slab * nt) * kDownCols;
-    const int all = g.f / kRingK, s0 = all * slab / g.slabs, s1 = all * (slab + 1) / g.slabs;   // slabs <= all
+    const int all = R::stages(g.f), s0 = all * slab / g.slabs, s1 = all * (slab + 1) / g.slabs;   // slabs <= all
+    const int K = (s1 < all ? kDownK * s1 : g.f) - kDownK * s0;
     const int e = pl.list[i], rows = __popc(pl.mask[e]), row0 = pl.row0[e];
     R ring;
-    ring.init([&](int r) { return (const bf16_t*)g.act + (size_t)(row0 + r) * g.f + s0 * kRingK; }, rows,
-              (const bf16_t*)g.wd + ((size_t)e * g.f + s0 * kRingK) * g.d + n0, nullptr, g.d, g.d - n0, s1 - s0);
+    ring.init([&](int r) { return (const bf16_t*)g.act + (size_t)(row0 + r) * g.f + s0 * kDownK; }, rows,
+              (const bf16_t*)g.wd + ((size_t)e * g.f + s0 * kDownK) * g.d + n0, nullptr, g.d, g.d - n0, K);
     layer_f32x16_t acc[R::kBlocks];
     ring.run(acc, smem, s1 - s0);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31;
@@ -640,18 +655,18 @@ extern "C" int xmoe_layer_few_fwd(const void* x, const void* w_router, const flo
     if (st != XMOE_OK) return st;
     const int active = (T * k < E ? T * k : E) + E_s;
     if (dt == XMOE_F32) return launch_alu<float>(a, active, s);
-    if (d % 64 || f % 64 || !aligned16(x) || !aligned16(wg) || !aligned16(wu) || !aligned16(wd))
+    if (d % 8 || f % 8 || !aligned16(x) || !aligned16(wg) || !aligned16(wu) || !aligned16(wd))
         return launch_alu<bf16_t>(a, active, s);
     // slabs of at least 8 stages until a token's experts alone give two blocks to every CU (the number of tokens has no say:
     // a token's bits are the same in every call)
     int down = (d + kDownCols - 1) / kDownCols;
-    while (a.slabs < kLayerSlabs && (k + E_s) * down * a.slabs < 512 && f / kRingK >= 16 * a.slabs) a.slabs *= 2;
+    while (a.slabs < kLayerSlabs && (k + E_s) * down * a.slabs < 512 && f >= 16 * kDownK * a.slabs) a.slabs *= 2;
     down *= a.slabs;
     if ((long)active * ((f + 127) / 128) >= kWideTiles)
-        XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<256, 4>), dim3((unsigned)(active * ((f + 127) / 128))),
+        XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<256, 32, 4>), dim3((unsigned)(active * ((f + 127) / 128))),
                                                           dim3(256), 0, s, a));
     else
-        XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<128, 6>), dim3((unsigned)(active * (f / 64))),
+        XMOE_LAUNCH(K_LAYER_UP_FEW, s, hipLaunchKernelGGL((layer_up_few_kernel<128, 64, 3>), dim3((unsigned)(active * ((f + 63) / 64))),
                                                           dim3(256), 0, s, a));
     XMOE_LAUNCH(K_LAYER_DOWN_FEW, s, hipLaunchKernelGGL(layer_down_few_kernel, dim3((unsigned)(active * down)), dim3(256), 0, s, a));
     return launch_layer_sum<bf16_t>(a, s);

@@ -17,7 +17,8 @@ DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 CASES = [(1, 64, 64, 8, 2, 0), (1, 2048, 192, 16, 6, 2), (2, 128, 192, 4, 4, 1), (3, 1003, 705, 16, 4, 1), (5, 50, 22, 7, 3, 2),
          (7, 7, 5, 3, 1, 0), (4, 3, 2, 5, 5, 1), (1, 1, 1, 1, 1, 0), (16, 320, 448, 64, 6, 2), (31, 72, 24, 6, 2, 0),
          (32, 64, 128, 1, 1, 1), (32, 256, 64, 12, 12, 3), (9, 520, 64, 512, 8, 0), (6, 136, 64, 300, 64, 1),
-         (2, 2048, 64, 257, 8, 1), (32, 192, 320, 40, 8, 2), (13, 65, 129, 24, 3, 0)]
+         (2, 2048, 64, 257, 8, 1), (32, 192, 320, 40, 8, 2), (13, 65, 129, 24, 3, 0),
+         (3, 1000, 712, 24, 3, 1), (8, 8, 8, 4, 2, 0), (11, 40, 1032, 9, 4, 1), (32, 264, 104, 5, 2, 2), (2, 904, 2056, 6, 2, 0)]
 
 
 def make(T, d, f, E, k, E_s, name, seed=0, std=0.1):
@@ -99,7 +100,7 @@ def test_against_the_oracle(case, name):
     c = make(*case, name)
     got, kernels = run(m, c)
     check(c, got)
-    matrix = name == "bf16" and c["d"] % 64 == 0 and c["f"] % 64 == 0
+    matrix = name == "bf16" and c["d"] % 8 == 0 and c["f"] % 8 == 0
     assert ("layer_up_few_kernel" in kernels) == matrix and ("layer_up_alu_kernel" in kernels) != matrix, kernels
 
 
