@@ -312,15 +312,17 @@ __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restric
 }
 
 // Threads of a row and vectors of a thread, for `vecs` 16-byte vectors of a row (CALL(threads, vectors)).  Few rows are
-// spread over more threads: a launch of few blocks waits for its loads, and more of them are in flight at once.
-#define XMOE_NORM_SHAPE(vecs, few, CALL)                         \
+// spread over more threads: a launch of few blocks waits for its loads, and more of them are in flight at once.  wide: rows of
+// up to 1024 vectors by as many threads (the backward, whose columns of dgain stay in registers).
+#define XMOE_NORM_SHAPE(vecs, few, wide, CALL)                   \
     do {                                                         \
         if ((vecs) <= 64) { CALL(64, 1); }                       \
         else if (!(few) && (vecs) <= 128) { CALL(64, 2); }       \
         else if (!(few) && (vecs) <= 256) { CALL(64, 4); }       \
         else if ((vecs) <= 256) { CALL(256, 1); }                \
         else if ((vecs) <= 512) { CALL(256, 2); }                \
-        else if ((vecs) <= 1024) { CALL(256, 4); }               \
+        else if (!(wide) && (vecs) <= 1024) { CALL(256, 4); }    \
+        else if ((vecs) <= 1024) { CALL(1024, 1); }              \
         else if ((vecs) <= 2048) { CALL(1024, 2); }              \
         else if constexpr (sizeof(T) == 4) { CALL(1024, 4); }    \
     } while (0)
@@ -338,7 +340,7 @@ int launch_norm(const void* x, const void* residual, const void* gain, int Tn, i
                                    dim3((unsigned)((Tn + norm_block(TPR) / TPR - 1) / (norm_block(TPR) / TPR))),       \
                                    dim3(norm_block(TPR)), 0, s, (const T*)x, (const T*)residual, (const T*)gain, Tn, d, \
                                    eps, (T*)h, (T*)y, (int8_t*)q, pitch, q_scale, rstd))
-    XMOE_NORM_SHAPE(cover, Tn <= kNormFewRows, XMOE_CALL);
+    XMOE_NORM_SHAPE(cover, Tn <= kNormFewRows, false, XMOE_CALL);
 #undef XMOE_CALL
     return XMOE_OK;
 }
@@ -346,13 +348,13 @@ int launch_norm(const void* x, const void* residual, const void* gain, int Tn, i
 template <typename T>
 int launch_norm_bwd(const void* dy, const void* dh, const void* h, const void* gain, const float* rstd, int Tn, int d,
                     void* dx, void* dgain, float* partial, hipStream_t s) {
-    const int vecs = (d + NormRow<T>::N - 1) / NormRow<T>::N, blocks = norm_bwd_blocks(Tn);
+    const int vecs = (d + NormRow<T>::N - 1) / NormRow<T>::N, blocks = norm_bwd_blocks(Tn, d);
     if (blocks > 0) {
 #define XMOE_CALL(TPR, NV)                                                                                              \
     XMOE_LAUNCH(K_ADD_RMSNORM_BWD, s,                                                                                   \
                 hipLaunchKernelGGL((add_rmsnorm_bwd_kernel<T, TPR, NV>), dim3((unsigned)blocks), dim3(norm_block(TPR)), 0, s, \
                                    (const T*)dy, (const T*)dh, (const T*)h, (const T*)gain, rstd, Tn, d, (T*)dx, partial))
-        XMOE_NORM_SHAPE(vecs, Tn <= kNormFewRows, XMOE_CALL);
+        XMOE_NORM_SHAPE(vecs, Tn <= kNormFewRows, true, XMOE_CALL);
 #undef XMOE_CALL
     }
     XMOE_LAUNCH(K_NORM_DGAIN, s,
