@@ -448,30 +448,33 @@ int launch_layer_sum(const LayerArgs& a, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// vector ALUs: float32, and bf16 widths that are no multiple of 64
+// vector ALUs: float32, and bf16 widths that are no multiple of 8
 // ---------------------------------------------------------------------------------------------------------
 // Thread (k-group of 16, column group c of 16): four consecutive k of every 64 and EV columns (16 bytes; one where N is less
 // than 16 bytes).  A column group that would pass N starts at N - EV instead: the columns it shares with its neighbour come
 // out the same twice.
-constexpr int kAluRows = 4;   // rows multiplied at a time
+// Rows multiplied at a time (R): 4, or 8 for the experts with more where EV is 4 (float32: acc holds 2 x 8 x 4 values; bf16's
+// EV = 8 would need 256 registers for it).
+template <int EV>
+constexpr int kAluRows = EV <= 4 ? 8 : 4;
 
-template <typename T, int M, int EV>
-__device__ __forceinline__ void alu_tile(const T* x, size_t ldx, const int (&src)[kAluRows], int K, const T* w0, const T* w1, int N,
-                                         int col, float (&acc)[M][kAluRows][EV]) {
+template <typename T, int M, int EV, int R>
+__device__ __forceinline__ void alu_tile(const T* x, size_t ldx, const int (&src)[R], int K, const T* w0, const T* w1, int N,
+                                         int col, float (&acc)[M][R][EV]) {
     const int kg = threadIdx.x >> 4;
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int r = 0; r < kAluRows; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int j = 0; j < EV; ++j) acc[m][r][j] = 0.f;
-    const T* xr[kAluRows];
+    const T* xr[R];
 #pragma unroll
-    for (int r = 0; r < kAluRows; ++r) xr[r] = x + (size_t)src[r] * ldx;
+    for (int r = 0; r < R; ++r) xr[r] = x + (size_t)src[r] * ldx;
     auto step = [&](int k0, auto part) {   // k0 .. k0 + 3, part: those below K
         constexpr bool kPart = decltype(part)::value;
         LayerVec<T, EV> w[M][4];
-        float a[kAluRows][4];
+        float a[R][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = kPart && k0 + i >= K ? K - 1 : k0 + i;
@@ -481,7 +484,7 @@ __device__ __forceinline__ void alu_tile(const T* x, size_t ldx, const int (&src
             }
         }
 #pragma unroll
-        for (int r = 0; r < kAluRows; ++r) {
+        for (int r = 0; r < R; ++r) {
             if (kPart) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) a[r][i] = to_float(xr[r][k0 + i < K ? k0 + i : K - 1]);
@@ -497,7 +500,7 @@ __device__ __forceinline__ void alu_tile(const T* x, size_t ldx, const int (&src
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int r = 0; r < kAluRows; ++r)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
                     for (int j = 0; j < EV; ++j) acc[m][r][j] = fmaf(a[r][i], to_float(w[m][i].v[j]), acc[m][r][j]);
         }
@@ -510,33 +513,33 @@ __device__ __forceinline__ void alu_tile(const T* x, size_t ldx, const int (&src
 
 // The block's tile of `cols` = 16 EV columns from n0 on: result(r, column, value of matrix 0, value of matrix 1) for every
 // row r < rows and column < N.  source(r): row r of x.
-template <typename T, int M, int EV, class Source, class Result>
-__device__ __forceinline__ void alu_product(const T* x, size_t ldx, int rows, int K, const T* w0, const T* w1, int N, int n0,
+template <typename T, int M, int EV, int R, class Source, class Result>
+__device__ __forceinline__ void alu_rows(const T* x, size_t ldx, int rows, int K, const T* w0, const T* w1, int N, int n0,
                                             float* red, Source source, Result result) {
     constexpr int C = 16 * EV;
     const int c = threadIdx.x & 15, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     int col = n0 + c * EV;
     if (col + EV > N) col = N - EV;
-    for (int r0 = 0; r0 < rows; r0 += kAluRows) {
-        int src[kAluRows];
+    for (int r0 = 0; r0 < rows; r0 += R) {
+        int src[R];
 #pragma unroll
-        for (int r = 0; r < kAluRows; ++r) src[r] = source(r0 + r < rows ? r0 + r : rows - 1);
-        float acc[M][kAluRows][EV];
-        alu_tile<T, M, EV>(x, ldx, src, K, w0, w1, N, col, acc);
+        for (int r = 0; r < R; ++r) src[r] = source(r0 + r < rows ? r0 + r : rows - 1);
+        float acc[M][R][EV];
+        alu_tile<T, M, EV, R>(x, ldx, src, K, w0, w1, N, col, acc);
         // the sixteen groups' sums: four of a wave, then the waves in order
 #pragma unroll
         for (int m = 0; m < M; ++m)
 #pragma unroll
-            for (int r = 0; r < kAluRows; ++r)
+            for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int j = 0; j < EV; ++j) {
                     float v = acc[m][r][j];
                     v += __shfl_xor(v, 16, 64);
                     v += __shfl_xor(v, 32, 64);
-                    if (lane < 16) red[((wave * M + m) * kAluRows + r) * C + c * EV + j] = v;
+                    if (lane < 16) red[((wave * M + m) * R + r) * C + c * EV + j] = v;
                 }
         __syncthreads();
-        for (int i = threadIdx.x; i < kAluRows * C; i += 256) {
+        for (int i = threadIdx.x; i < R * C; i += 256) {
             const int r = i / C, cc = i - r * C;
             int at = n0 + cc / EV * EV;   // where the column group of this sum starts
             if (at + EV > N) at = N - EV;
@@ -545,17 +548,25 @@ __device__ __forceinline__ void alu_product(const T* x, size_t ldx, int rows, in
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v[m] += red[((w * M + m) * kAluRows + r) * C + cc];
+                for (int w = 0; w < 4; ++w) v[m] += red[((w * M + m) * R + r) * C + cc];
             if (r0 + r < rows && at < N) result(r0 + r, at, v[0], v[1]);
         }
         __syncthreads();
     }
 }
+template <typename T, int M, int EV, class Source, class Result>
+__device__ __forceinline__ void alu_product(const T* x, size_t ldx, int rows, int K, const T* w0, const T* w1, int N, int n0,
+                                            float* red, Source source, Result result) {
+    if (kAluRows<EV> > 4 && rows > 4)
+        alu_rows<T, M, EV, kAluRows<EV>>(x, ldx, rows, K, w0, w1, N, n0, red, source, result);
+    else
+        alu_rows<T, M, EV, 4>(x, ldx, rows, K, w0, w1, N, n0, red, source, result);
+}
 
 template <typename T, int EV>
 __global__ __launch_bounds__(256) void layer_up_alu_kernel(LayerArgs g) {
     constexpr int C = 16 * EV;
-    __shared__ float red[4 * 2 * kAluRows * C];
+    __shared__ float red[4 * 2 * kAluRows<EV> * C];
     __shared__ LayerPlan pl;
     layer_plan(pl, g);
     if (blockIdx.x == 0) layer_rows(pl, g);
@@ -573,7 +584,7 @@ __global__ __launch_bounds__(256) void layer_up_alu_kernel(LayerArgs g) {
 template <typename T, int EV>
 __global__ __launch_bounds__(256) void layer_down_alu_kernel(LayerArgs g) {
     constexpr int C = 16 * EV;
-    __shared__ float red[4 * kAluRows * C];
+    __shared__ float red[4 * kAluRows<EV> * C];
     __shared__ LayerPlan pl;
     layer_plan(pl, g);
     const int nt = (g.d + C - 1) / C, i = blockIdx.x / nt, tile = blockIdx.x - i * nt;
