@@ -80,6 +80,7 @@ const char* const kKernelNames[K_COUNT] = {
     "q8_rows_kernel",
     "q8_down_kernel",
     "q8_gateup_few_kernel",
+    "q8_down_few_kernel",
     "layer_route_kernel",
     "layer_up_few_kernel",
     "layer_down_few_kernel",

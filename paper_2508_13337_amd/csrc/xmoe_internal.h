@@ -72,6 +72,7 @@ enum KernelId : int {
     K_Q8_ROWS,
     K_Q8_DOWN,
     K_Q8_GATEUP_FEW,
+    K_Q8_DOWN_FEW,
     K_LAYER_ROUTE,
     K_LAYER_UP_FEW,
     K_LAYER_DOWN_FEW,

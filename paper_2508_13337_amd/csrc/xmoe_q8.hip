@@ -136,6 +136,19 @@ __device__ __forceinline__ void q8_store4(float* __restrict__ row, int col, int 
         if (col + i < N) row[col + i] = s[i];
 }
 
+struct __attribute__((packed, aligned(2))) Q8B4 {
+    uint32_t v[2];
+};
+__device__ __forceinline__ void q8_store4(bf16_t* __restrict__ row, int col, int N, const float (&s)[4]) {
+    if (col + 4 <= N) {
+        *reinterpret_cast<Q8B4*>(row + col) = Q8B4{{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])}};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col + i < N) row[col + i] = from_float<bf16_t>(s[i]);
+}
+
 struct Q8Args {
     const int8_t* x;            // rows, pitch bytes each
     const float* x_scale;       // of a row
@@ -418,13 +431,15 @@ int launch_q8_down(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
 }
 
 // =========================================================================================================
-// Gate and up of few rows (a decoding step): the weights' bytes are the bound.  32 rows and 64 columns of either matrix per
-// block of 4 waves, two blocks per CU.  A stage is 256 k, two cache lines of each row (one line of each costs memory a
-// tenth of its rate); two stages of 40 KiB, the second on its way while the first is multiplied.  Waves 0, 1 and 2, 3 take
-// half of a stage's k each, and their sums, which are integers, are added in LDS.  (Straight from memory to registers, 32
-// bytes of 32 rows at a time: slower by a quarter, the loads' addresses take the L1 cache too long.)
+// Few rows (a decoding step): the weights' bytes are the bound.  32 rows and 64 columns (gate/up: of either matrix) per block
+// of 4 waves.  A stage is 256 k, two cache lines of each row (one line of each costs memory a tenth of its rate); two stages,
+// the second on its way while the first is multiplied, 40 KiB each for gate/up (two blocks per CU), 24 for down (three).
+// Waves 0, 1 and 2, 3 take half of a stage's k each, and their sums, which are integers, are added in LDS.  Tried: straight
+// from memory to registers, 32 bytes of 32 rows at a time (slower by a quarter, the loads' addresses take the L1 cache too
+// long); 128 columns for down (34 experts, d 2048, f 1408: 29 us for 23, too few blocks for an even load); 32 for gate/up (51
+// for 48); 64 rows (one block per CU: 95 for 76).  Measured, d 2048, f 1408, 37 of 66 experts with one or two rows each:
+// gate/up 44 us (4.8 TB/s), down 23 (4.6); all 66: 72 (5.3) and 39 (4.9).
 // =========================================================================================================
-constexpr int kFewW = 128 * 256, kFewX = 32 * 256, kFewStage = kFewW + kFewX;
 __device__ __align__(16) const uint32_t kQ8Zero[4] = {0u, 0u, 0u, 0u};
 
 // A lane's pieces of the wave's share of an operand's stage ([rows][256 bytes]), 4 rows per load, piece (lane % 16) XOR-ed with
@@ -444,9 +459,11 @@ struct Few8Rows {
             upper |= (uint32_t)(c >> 3) << i;
         }
     }
-    __device__ __forceinline__ void issue(char* __restrict__ unit, int first, bool half) {   // half: K ends in the middle
+    // half: K ends in the middle.  Four rows none of which is below `rows` are left out.
+    __device__ __forceinline__ void issue(char* __restrict__ unit, int first, int rows, bool half) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
+            if (first + i * 4 >= rows) break;
             const bool out = half && ((upper >> i) & 1u);
             q8_load16(out ? reinterpret_cast<const int8_t*>(kQ8Zero) : p[i], unit + (first + i * 4) * 256);
             p[i] += 256;
@@ -457,80 +474,85 @@ __device__ __forceinline__ q8_i32x4_t few8_frag(const char* unit, int base, int 
     const int lane = threadIdx.x & 63, r = base + (lane & 31), c = 2 * ks + (lane >> 5);
     return *reinterpret_cast<const q8_i32x4_t*>(unit + r * 256 + ((c ^ (r & 15)) << 4));
 }
-__device__ __forceinline__ void few8_stage(q8_i32x16_t (&acc)[2], Few8Rows<8>& w, Few8Rows<2>& x, bool more, bool half,
-                                           char* __restrict__ next, const char* __restrict__ cur) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = wave & 1, wk = wave >> 1;
-    if (more) {
-        w.issue(next, wave * 32, half);
-        x.issue(next + kFewW, wave * 8, half);
+// Stages of 64 NB weight rows and 32 rows of x.  Wave (wn = wave % 2, wk = wave / 2): weight rows 64 n + 32 wn .. + 31 of every
+// n < NB, all of x, half wk of a stage's k.
+template <int NB>
+struct Few8 {
+    static constexpr int kW = NB * 64 * 256, kStage = kW + 32 * 256;
+    Few8Rows<4 * NB> w;
+    Few8Rows<2> x;
+    q8_i32x16_t acc[NB];
+    __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    __device__ __forceinline__ void issue(char* __restrict__ stage, int rows, bool half) {
+        w.issue(stage, wave() * 16 * NB, 64 * NB, half);
+        x.issue(stage + kW, wave() * 8, rows, half);
     }
+    __device__ __forceinline__ void stage(int rows, bool more, bool half, char* __restrict__ next, const char* __restrict__ cur) {
+        const int wn = wave() & 1, wk = wave() >> 1;
+        if (more) issue(next, rows, half);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int ks = 4 * wk + i;
-        const q8_i32x4_t a = few8_frag(cur + kFewW, 0, ks);
+        for (int i = 0; i < 4; ++i) {
+            const int ks = 4 * wk + i;
+            const q8_i32x4_t a = few8_frag(cur + kW, 0, ks);
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-            acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(few8_frag(cur, 64 * n + 32 * wn, ks), a,
-                                                           acc[n], 0, 0, 0);
+            for (int n = 0; n < NB; ++n)
+                acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(few8_frag(cur, 64 * n + 32 * wn, ks), a, acc[n], 0, 0, 0);
+        }
     }
-}
-// The sums of the block's rows and columns; of all waves, 0 and 1 have them.
-__device__ __forceinline__ void few8_product(q8_i32x16_t (&acc)[2], Few8Rows<8>& w, Few8Rows<2>& x, int pitch, char* smem) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int stages = (pitch + 255) / 256;
-    const bool tail = pitch % 256 != 0;
+    // Rows of x from `rows` on hold anything.  The waves' sums of half of k, in LDS, are added by sum().
+    __device__ __forceinline__ void product(int pitch, int rows, char* smem) {
+        const int stages = (pitch + 255) / 256;
+        const bool tail = pitch % 256 != 0;
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[n][v] = 0;
-    w.issue(smem, wave * 32, tail && stages == 1);
-    x.issue(smem + kFewW, wave * 8, tail && stages == 1);
-    for (int s = 0; s < stages; ++s) {
-        q8_wait_and_barrier<0>();   // stage s has landed for every thread, and every wave is done with stage s - 1
-        char* cur = smem + (s & 1) * kFewStage;
-        few8_stage(acc, w, x, s + 1 < stages, tail && s + 2 == stages, smem + ((s + 1) & 1) * kFewStage, cur);
+            for (int v = 0; v < 16; ++v) acc[n][v] = 0;
+        issue(smem, rows, tail && stages == 1);
+        for (int s = 0; s < stages; ++s) {
+            q8_wait_and_barrier<0>();   // stage s has landed for every thread, and every wave is done with stage s - 1
+            stage(rows, s + 1 < stages, tail && s + 2 == stages, smem + ((s + 1) & 1) * kStage, smem + (s & 1) * kStage);
+        }
+        __syncthreads();
+        int* red = reinterpret_cast<int*>(smem) + wave() * (NB * 1024) + (threadIdx.x & 63);
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) red[(n * 16 + v) * 64] = acc[n][v];
+        __syncthreads();
     }
-    __syncthreads();
-    int* red = reinterpret_cast<int*>(smem) + (wave & 1) * 2048;
-    if (wave >= 2) {
+    // weight rows 64 n + 32 wn ..
+    __device__ __forceinline__ static q8_i32x16_t sum(const char* smem, int n, int wn) {
+        const int* red = reinterpret_cast<const int*>(smem) + (wn * NB + n) * 1024 + (threadIdx.x & 63);
+        q8_i32x16_t a;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) red[(n * 16 + v) * 64 + lane] = acc[n][v];
+        for (int v = 0; v < 16; ++v) a[v] = red[v * 64] + red[2 * NB * 1024 + v * 64];
+        return a;
     }
-    __syncthreads();
-    if (wave < 2) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[n][v] += red[(n * 16 + v) * 64 + lane];
-    }
-}
+};
 
 __global__ __launch_bounds__(256, 2) void q8_gateup_few_kernel(Q8Args g) {
-    __shared__ __align__(16) char smem[2 * kFewStage];
+    typedef Few8<2> F;
+    __shared__ __align__(16) char smem[2 * F::kStage];
     Q8Tile t;
     if (!t.place(g, 64)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, r = lane & 31;
-    Few8Rows<8> w;
-    Few8Rows<2> x;
-    w.init(wave < 2 ? g.w0 : g.w1, g.pitch, wave * 32, [&](int c) {
+    const int lane = threadIdx.x & 63, wave = F::wave(), half = lane >> 5;
+    F p;
+    p.w.init(wave < 2 ? g.w0 : g.w1, g.pitch, wave * 32, [&](int c) {
         const int n = t.n0 + (c & 63);
         return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
     });
-    x.init(g.x, g.pitch, wave * 8, [&](int i) {
+    p.x.init(g.x, g.pitch, wave * 8, [&](int i) {
         i = t.row0 + (i < t.rows ? i : t.rows - 1);
         return g.row_index ? g.row_index[i] : i;
     });
-    const int row = t.row0 + (r < t.rows ? r : t.rows - 1), c0 = t.n0 + 32 * (wave & 1);
+    const int r = lane & 31, row = t.row0 + (r < t.rows ? r : t.rows - 1), c0 = t.n0 + 32 * (wave & 1);
     float xs = g.x_scale[g.row_index ? g.row_index[row] : row], gs[4][4], us[4][4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         q8_scales(g.s0 + (size_t)t.e * g.N, c0 + 4 * half + 8 * q, g.N, gs[q]);
         q8_scales(g.s1 + (size_t)t.e * g.N, c0 + 4 * half + 8 * q, g.N, us[q]);
     }
-    q8_i32x16_t acc[2];
-    few8_product(acc, w, x, g.pitch, smem);
+    p.product(g.pitch, t.rows, smem);
     if (wave >= 2) return;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -538,16 +560,53 @@ __global__ __launch_bounds__(256, 2) void q8_gateup_few_kernel(Q8Args g) {
         us[v / 4][v % 4] *= 1.0f / kLog2e;
     }
     uint2 o[4];
-    const float m = q8_activation(acc[0], acc[1], xs, gs, us, o);
+    const float m = q8_activation(F::sum(smem, 0, wave & 1), F::sum(smem, 1, wave & 1), xs, gs, us, o);
     if (r >= t.rows) return;
     if (half == 0) g.gmax[(size_t)row * (g.a_pitch / kQ8Group) + c0 / kQ8Group] = m;
 #pragma unroll
     for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(g.a16 + (size_t)row * g.a_pitch + c0 + 4 * half + 8 * q) = o[q];
 }
 
+template <typename T>
+__global__ __launch_bounds__(256, 2) void q8_down_few_kernel(Q8Args g) {
+    typedef Few8<1> F;
+    __shared__ __align__(16) char smem[2 * F::kStage];
+    Q8Tile t;
+    if (!t.place(g, 64)) return;
+    const int lane = threadIdx.x & 63, wave = F::wave();
+    F p;
+    p.w.init(g.w0, g.pitch, wave * 16, [&](int c) {
+        const int n = t.n0 + c;
+        return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
+    });
+    p.x.init(g.x, g.pitch, wave * 8, [&](int i) { return t.row0 + (i < t.rows ? i : t.rows - 1); });
+    const int r = lane & 31, row = t.row0 + (r < t.rows ? r : t.rows - 1);
+    const float as = g.x_scale[row];
+    p.product(g.pitch, t.rows, smem);
+    if (wave >= 2 || r >= t.rows) return;
+    const q8_i32x16_t sum = F::sum(smem, 0, wave & 1);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int col = t.n0 + 32 * wave + 8 * q + 4 * (lane >> 5);
+        float s[4], o[4];
+        q8_scales(g.s0 + (size_t)t.e * g.N, col, g.N, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = (float)sum[4 * q + i] * (as * s[i]);
+        q8_store4((T*)g.y + (size_t)row * g.N, col, g.N, o);
+    }
+}
+
 int launch_q8_gateup_few(const Q8Args& a, int max_tiles, hipStream_t s) {
     XMOE_LAUNCH(K_Q8_GATEUP_FEW, s, hipLaunchKernelGGL(q8_gateup_few_kernel, dim3((unsigned)q8_blocks(a.N, 64, max_tiles)),
                                                        dim3(256), 0, s, a));
+    return XMOE_OK;
+}
+int launch_q8_down_few(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
+    const dim3 grid((unsigned)q8_blocks(a.N, 64, max_tiles)), block(256);
+    if (dt == XMOE_F32)
+        XMOE_LAUNCH(K_Q8_DOWN_FEW, s, hipLaunchKernelGGL(q8_down_few_kernel<float>, grid, block, 0, s, a));
+    else
+        XMOE_LAUNCH(K_Q8_DOWN_FEW, s, hipLaunchKernelGGL(q8_down_few_kernel<bf16_t>, grid, block, 0, s, a));
     return XMOE_OK;
 }
 
@@ -636,9 +695,10 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restri
 }
 
 
-// Rows of a tile, by the mean load.  Measured (MI355X, all launches together, us, 256 | 128 | 32 with 128-row down tiles):
+// Rows of a tile, by the mean load.  Measured (MI355X, all launches together, us, 256 | 128 | 32):
 //     mean rows                           1 - 2         8          16         62        124       248       500       1000
-//     64 experts + 2, d 2048, f 1408    122|99|92   177|146|141    - |153|156  197|179   236|202   281|290   479|490   834|885
+//     64 experts + 2, d 2048, f 1408    122|99|88   177|146|131    - |152|142  197|177   236|200   281|290   479|490   834|885
+//     (32-row tiles at 31 and 47 mean rows: 155 for 156, 190 for 171; 8 experts, f 14336, 32 mean rows: 393 for 341)
 //     8 experts, d 2048, f 1408              (4) - |44|43           - |44|42    62|44     70|50     75|60     84|92   239|237 (2048)
 //     256 experts, d 2048, f 512        - |185|171       -         - |218|205  292|244   346|322   497|485
 //     64 experts, d 2048, Zipf load                                            186|171 (96)  260|253 (192)  431|407 (384)
@@ -702,14 +762,16 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
                        g_scale, u_scale, dp, f, tile_rows, a16, gmax, fp, nullptr};
     const Q8Args down = {aq, as, nullptr, expert_offsets, map, (const int8_t*)wdq, nullptr, d_scale, nullptr, fp, d, tile_rows,
                          nullptr, nullptr, 0, y};
-    st = tile_rows == 256 ? launch_q8_gateup<256, 8>(up, max_tiles, s)
+    st = tile_rows == 256   ? launch_q8_gateup<256, 8>(up, max_tiles, s)
          : tile_rows == 128 ? launch_q8_gateup<128, 4>(up, max_tiles, s)
                             : launch_q8_gateup_few(up, max_tiles, s);
     if (st != XMOE_OK) return st;
     XMOE_LAUNCH(K_Q8_ROWS, s,
                 hipLaunchKernelGGL(q8_rows_kernel, dim3((unsigned)((B + 3) / 4)), dim3(256), 0, s, a16, gmax, expert_offsets,
                                    E, f, fp, aq, as));
-    return tile_rows == 256 ? launch_q8_down<256, 8>(down, max_tiles, dt, s) : launch_q8_down<128, 4>(down, max_tiles, dt, s);
+    return tile_rows == 256   ? launch_q8_down<256, 8>(down, max_tiles, dt, s)
+           : tile_rows == 128 ? launch_q8_down<128, 4>(down, max_tiles, dt, s)
+                              : launch_q8_down_few(down, max_tiles, dt, s);
 }
 
 }  // extern "C"
