@@ -35,6 +35,14 @@ __device__ __forceinline__ void q8_wait_and_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The thread's number, anew: what follows from it inside a loop over tiles is computed there, not held in registers over the
+// products
+__device__ __forceinline__ int q8_tid() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 // A lane's pieces of the wave's share of an operand unit ([rows][128 bytes of k]): 8 rows per load, piece (lane % 8) XOR-ed
 // with (row / 2) % 8, so that a fragment read falls on all banks.  Units are requested in order; behind the last one of K
 // that one is fetched again, which keeps the wait counts uniform, and not used.
@@ -44,7 +52,7 @@ struct Q8Rows {
     // row r of the operand is at base + source(r) * pitch
     template <class Source>
     __device__ __forceinline__ void init(const int8_t* base, size_t pitch, int first, Source source) {
-        const int lane = threadIdx.x & 63;
+        const int lane = q8_tid() & 63;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = first + i * 8 + (lane >> 3);
@@ -157,22 +165,30 @@ struct Q8Args {
     const int8_t *w0, *w1;      // [E, N, pitch]; w1: up
     const float *s0, *s1;       // [E, N]
     int pitch, N, tile_rows;    // tile_rows: the tile map's
+    int group;                  // row tiles that go through the column tiles together
     int16_t* a16;               // gate/up: [rows][a_pitch]
     float* gmax;                // [rows][a_pitch / 32]
     int a_pitch;
     void* y;                    // down: [rows][N]
 };
 
-// The block's tile: row tiles x column tiles, column tiles of a row tile in a run, the runs dealt to the XCDs in eight parts
-// of equal length (workgroup L goes to XCD L % 8): the tiles of an expert share their weights and rows in one L2.
+// Row tiles that go through the column tiles together.  The 32 CUs of an XCD then read 4 + 8 operand tiles at a time, not 1 + 32
+// (d 4096, f 14336, 8 experts with 512 rows each: 997 us, in twos 952, in fours 939, in eights 936; d 2048, f 1408, 66 with 500:
+// 464, 431, 427, 424).
+constexpr int kQ8RowTiles = 4;
+// Tile L: row tiles x column tiles, in groups of `group` row tiles (those of a column tile, then the next column tile), dealt to
+// the XCDs in eight runs of equal length (workgroup L goes to XCD L % 8): tiles in flight together share their weights
+// and rows in one L2.
 struct Q8Tile {
     int e, row0, rows, n0;
-    __device__ __forceinline__ bool place(const Q8Args& a, int cols) {
+    __device__ __forceinline__ bool place(const Q8Args& a, int cols, int group, long L) {
         const int nt = (a.N + cols - 1) / cols;
-        const long total = (long)a.map[0] * nt, run = (total + 7) / 8, slot = blockIdx.x >> 3, t = (blockIdx.x & 7) * run + slot;
+        const long total = (long)a.map[0] * nt, run = (total + 7) / 8, slot = L >> 3, t = (L & 7) * run + slot;
         if (slot >= run || t >= total) return false;
-        const int tile = (int)(t / nt);
-        n0 = (int)(t - (long)tile * nt) * cols;
+        const int g0 = (int)(t / ((long)nt * group)) * group, in = (int)(t - (long)g0 * nt);
+        const int rows_of_group = a.map[0] - g0 < group ? a.map[0] - g0 : group;
+        const int tile = g0 + in % rows_of_group;
+        n0 = in / rows_of_group * cols;
         e = a.map[4 + 2 * tile];
         row0 = a.map[4 + 2 * tile + 1];
         rows = a.off[e + 1] - row0;
@@ -186,30 +202,31 @@ long q8_blocks(int N, int cols, int max_tiles) { return ((long)max_tiles * ((N +
 // =========================================================================================================
 // Tiles of MT x MT (gate/up: the same MT / 2 columns of both).  Units A(0) B(0) A(1) B(1) .. of MT rows x 128 k run through
 // five slots, two to three of them on their way.
-//   256: 8 waves (2 x 4) of 128 x 64 each, 160 KiB, one block per CU: the most products per byte of LDS
+//   256: 8 waves (2 x 4) of 128 x 64 each, 160 KiB, one block per CU: the most products per byte of LDS.  A block takes tile
+//        after tile, and the units of the next one follow those of this one without a pause (against a block per tile: down
+//        264 us -> 247, gate/up 487 -> 481, with the order of the tiles 465; 66 experts, d 2048, f 1408, 993 mean rows: 1.63
+//        POP/s of the 2.08 of a large library product.  LDS reads and MFMA both take about half of the loop's time.)
 //   128: 4 waves (2 x 2) of 64 x 64 each, 80 KiB, two blocks per CU: where the weights' bytes are the bound, or 256 rows few
 // =========================================================================================================
 template <int MT, int WAVES>
 struct Tile8 {
     static constexpr int kWaves = WAVES, kThreads = 64 * WAVES, kWn = WAVES / 2, kMi = MT / 64, kNi = MT / 32 / kWn,
                          kLoads = MT / 8 / WAVES, kUnit = MT * 128, kLds = 5 * kUnit;
+    static constexpr bool kRoll = MT == 256;
+    static constexpr int kCols = MT / 2, kPieces = kCols / 8;   // columns of a 32-column block of all waves; 16-byte pieces
     typedef q8_i32x16_t Acc[kMi][kNi];
     __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
     __device__ __forceinline__ static int wm() { return wave() / kWn; }
     __device__ __forceinline__ static int wn() { return wave() % kWn; }
     __device__ __forceinline__ static int first() { return wave() * 8 * kLoads; }   // row of the wave's share of a unit
-    // first column of the wave's ni-th 32 (DUAL: the first half of them of the first matrix), first row of its mi-th
-    template <bool DUAL>
-    __device__ __forceinline__ static int col(int ni) {
-        constexpr int H = kNi / 2;
-        return DUAL ? ni / H * (MT / 2) + wn() * 32 * H + ni % H * 32 : wn() * 32 * kNi + ni * 32;
-    }
+    // first column of the wave's ni-th 32, first row of its mi-th
+    __device__ __forceinline__ static int col(int ni) { return ni * kCols + wn() * 32; }
     __device__ __forceinline__ static int row(int mi) { return wm() * (MT / 2) + mi * 32; }
 };
-template <class W, bool DUAL, int MI>
+template <class W, int MI>
 __device__ __forceinline__ void tile8_read(Q8Frags<MI, W::kNi>& f, const char* ua, const char* ub, int ks) {
 #pragma unroll
-    for (int ni = 0; ni < W::kNi; ++ni) f.b[ni] = q8_frag(ub, W::template col<DUAL>(ni), ks);
+    for (int ni = 0; ni < W::kNi; ++ni) f.b[ni] = q8_frag(ub, W::col(ni), ks);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) f.a[mi] = q8_frag(ua, W::row(mi), ks);
 }
@@ -224,28 +241,32 @@ __device__ __forceinline__ void q8_mma(q8_i32x16_t (&acc)[N][NI], const Q8Frags<
 // One pass: the four steps on A(p) = ua, B(p) = ub.  On entry both have landed, every wave has left the units of pass p - 1
 // (fill1, fill2), and f1 holds that pass's last step.  The slots are distinct, and saying so matters: an LDS read that may
 // observe a direct-to-LDS load in flight makes the compiler wait for all of them.
-template <class W, bool DUAL, int MI>
+template <class W, int MI>
 __device__ __forceinline__ void tile8_pass(typename W::Acc& acc, Q8Frags<MI, W::kNi>& f0, Q8Frags<MI, W::kNi>& f1,
                                            Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, bool more_a, bool more_b,
                                            char* __restrict__ fill1, char* __restrict__ fill2,
                                            const char* __restrict__ ua, const char* __restrict__ ub) {
     b.issue(fill1, W::first(), more_b);  // B(p+1)
     __builtin_amdgcn_sched_barrier(0);   // the requests stay where they stand: sunk to the end of the pass they are late
-    tile8_read<W, DUAL, MI>(f0, ua, ub, 0);
+    tile8_read<W, MI>(f0, ua, ub, 0);
     q8_mma(acc, f1);
-    tile8_read<W, DUAL, MI>(f1, ua, ub, 1);
+    tile8_read<W, MI>(f1, ua, ub, 1);
     q8_mma(acc, f0);
     __builtin_amdgcn_sched_barrier(0);
     a.issue(fill2, W::first(), more_a);  // A(p+2)
     __builtin_amdgcn_sched_barrier(0);
-    tile8_read<W, DUAL, MI>(f0, ua, ub, 2);
+    tile8_read<W, MI>(f0, ua, ub, 2);
     q8_mma(acc, f1);
-    tile8_read<W, DUAL, MI>(f1, ua, ub, 3);
+    tile8_read<W, MI>(f1, ua, ub, 3);
     q8_mma(acc, f0);
 }
-// MI: the wave's 32-row blocks that hold rows (0: it only takes part in the loads)
-template <class W, bool DUAL, int MI>
-__device__ __forceinline__ void tile8_loop(typename W::Acc& acc, Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, int np, char* smem) {
+__device__ __forceinline__ int q8_slot(int s) { return s < 5 ? s : s - 5; }
+// MI: the wave's 32-row blocks that hold rows (0: it only takes part in the loads).  sa: slot of A(0), then of the pass.
+// Where tiles follow one another (W::kRoll) the units behind the last one are the next tile's first: next_a() and next_b()
+// turn to it.
+template <class W, int MI, class NextA, class NextB>
+__device__ __forceinline__ void tile8_loop(typename W::Acc& acc, Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, int np, char* smem,
+                                           int& sa, NextA next_a, NextB next_b) {
     constexpr int kUnit = W::kUnit, M = MI > 0 ? MI : 1;
     const q8_i32x4_t z = {0, 0, 0, 0};
     Q8Frags<M, W::kNi> f0, f1;
@@ -253,176 +274,248 @@ __device__ __forceinline__ void tile8_loop(typename W::Acc& acc, Q8Rows<W::kLoad
     for (int mi = 0; mi < M; ++mi) f1.a[mi] = z;
 #pragma unroll
     for (int ni = 0; ni < W::kNi; ++ni) f1.b[ni] = z;
-    int sa = 0;   // slot of A(p) = 2p % 5
+#pragma nounroll
     for (int p = 0; p < np; ++p) {
-        const int sb = sa + 1 < 5 ? sa + 1 : sa - 4, s3 = sa + 3 < 5 ? sa + 3 : sa - 2, s4 = sa + 4 < 5 ? sa + 4 : sa - 1;
+        const int sb = q8_slot(sa + 1), s3 = q8_slot(sa + 3), s4 = q8_slot(sa + 4);
+        if (W::kRoll && p + 2 == np) next_a();
+        if (W::kRoll && p + 1 == np) next_b();
+        __builtin_amdgcn_sched_barrier(0);
+        const bool more_a = W::kRoll || p + 3 < np, more_b = W::kRoll || p + 2 < np;
         if (MI > 0) {
-            tile8_pass<W, DUAL, M>(acc, f0, f1, a, b, p + 3 < np, p + 2 < np, smem + s3 * kUnit, smem + s4 * kUnit,
-                                   smem + sa * kUnit, smem + sb * kUnit);
+            tile8_pass<W, M>(acc, f0, f1, a, b, more_a, more_b, smem + s3 * kUnit, smem + s4 * kUnit, smem + sa * kUnit,
+                             smem + sb * kUnit);
         } else {
-            b.issue(smem + s3 * kUnit, W::first(), p + 2 < np);
-            a.issue(smem + s4 * kUnit, W::first(), p + 3 < np);
+            b.issue(smem + s3 * kUnit, W::first(), more_b);
+            a.issue(smem + s4 * kUnit, W::first(), more_a);
         }
         q8_wait_and_barrier<W::kLoads>();
-        sa = sa + 2 < 5 ? sa + 2 : sa - 3;
+        sa = q8_slot(sa + 2);
     }
     if (MI > 0) q8_mma(acc, f1);
 }
-// rows: valid ones of the tile, which may exceed it
-template <class W, bool DUAL>
+// The tile's sums.  rows: valid ones of the tile, which may exceed it
+template <class W, class NextA, class NextB>
 __device__ __forceinline__ void tile8_product(typename W::Acc& acc, Q8Rows<W::kLoads>& a, Q8Rows<W::kLoads>& b, int np, int rows,
-                                              char* smem) {
-    constexpr int kUnit = W::kUnit;
+                                              char* smem, int& sa, NextA next_a, NextB next_b) {
 #pragma unroll
     for (int mi = 0; mi < W::kMi; ++mi)
 #pragma unroll
         for (int ni = 0; ni < W::kNi; ++ni)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0;
-    a.issue(smem, W::first(), np > 1);
-    b.issue(smem + kUnit, W::first(), np > 1);
-    a.issue(smem + 2 * kUnit, W::first(), np > 2);
-    // at the top of pass p everything up to B(p) has landed for every thread, A(p+1) may be on its way
-    q8_wait_and_barrier<W::kLoads>();
     const int left = rows - W::row(0);
     if (left <= 0)
-        tile8_loop<W, DUAL, 0>(acc, a, b, np, smem);
+        tile8_loop<W, 0>(acc, a, b, np, smem, sa, next_a, next_b);
     else if (W::kMi == 2 && left <= 32)
-        tile8_loop<W, DUAL, 1>(acc, a, b, np, smem);
+        tile8_loop<W, 1>(acc, a, b, np, smem, sa, next_a, next_b);
     else
-        tile8_loop<W, DUAL, W::kMi>(acc, a, b, np, smem);
-    q8_wait_and_barrier<0>();   // nothing may land in this LDS any more: it becomes the results'
+        tile8_loop<W, W::kMi>(acc, a, b, np, smem, sa, next_a, next_b);
+    if (!W::kRoll) q8_wait_and_barrier<0>();   // nothing may land in this LDS any more: it becomes the results'
+}
+// The block's tiles: one, or (kRoll) every gridDim-th.  rows_of(t, i): row of g.x of the tile's i-th;  weights(t, i): the tile's
+// i-th row of weights;  results(t, acc, at): at(r) is row r of MT / 2 columns of 16 bits in LDS that is free: the two units of
+// the last pass, those behind hold the next tile's.
+template <class W, class RowIndex, class Weights, class Ahead, class Results>
+__device__ __forceinline__ void tile8_run(const Q8Args& g, int cols, char* smem, RowIndex row_index, Weights weights, Ahead ahead,
+                                          Results results) {
+    Q8Tile t, next;
+    long L = blockIdx.x;
+    if (!t.place(g, cols, g.group, L)) return;
+    const int np = g.pitch / 128;
+    Q8Rows<W::kLoads> a, b;
+    int src[W::kLoads];   // rows of the A units to come
+    auto fetch_rows = [&](const Q8Tile& u) {
+        const int r0 = W::first() + ((q8_tid() & 63) >> 3);
+#pragma unroll
+        for (int i = 0; i < W::kLoads; ++i) src[i] = row_index(u, r0 + 8 * i);
+    };
+    auto turn_a = [&] {
+        int i = 0;
+        a.init(g.x, g.pitch, W::first(), [&](int) { return src[i++]; });
+    };
+    fetch_rows(t);
+    turn_a();
+    weights(t, b);
+    a.issue(smem, W::first(), np > 1);
+    b.issue(smem + W::kUnit, W::first(), np > 1 || W::kRoll);
+    a.issue(smem + 2 * W::kUnit, W::first(), np > 2 || W::kRoll);
+    // at the top of pass p everything up to B(p) has landed for every thread, A(p+1) may be on its way
+    q8_wait_and_barrier<W::kLoads>();
+    int sa = 0;
+    for (;;) {
+        L += gridDim.x;
+        const bool more = W::kRoll && next.place(g, cols, g.group, L);
+        if (!more) next = t;   // its units are requested again, and not used
+        if (W::kRoll) fetch_rows(next);
+        ahead(t);
+        typename W::Acc acc;
+        tile8_product<W>(acc, a, b, np, t.rows, smem, sa, turn_a, [&] { weights(next, b); });
+        char *res0 = smem + (W::kRoll ? q8_slot(sa + 3) : 0) * W::kUnit, *res1 = smem + (W::kRoll ? q8_slot(sa + 4) : 1) * W::kUnit;
+        __builtin_amdgcn_sched_barrier(0);
+        results(t, acc, res0, res1);
+        if (!more) break;
+        t = next;
+    }
+    if (W::kRoll) q8_wait_and_barrier<0>();
+}
+// LDS writes done and seen, or LDS reads returned: direct-to-LDS loads go on
+__device__ __forceinline__ void q8_lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A 16-byte piece c of row r of results, pieces XOR-ed with the row.  u0, u1: units of 128 rows of 256 bytes, or of 128 of 128
+template <class W>
+__device__ __forceinline__ char* tile8_at(char* u0, char* u1, int r, int c) {
+    return (r < 128 ? u0 : u1) + (r & 127) * (2 * W::kCols) + ((c ^ (r & (W::kPieces - 1))) << 4);
+}
+// store(r, c, piece c of row r) for the pieces in LDS of all rows below `rows`
+template <class W, class Store>
+__device__ __forceinline__ void tile8_store(char* u0, char* u1, int rows, Store store) {
+    constexpr int kStep = W::kThreads / W::kPieces, kRows = W::kMi * 64;
+    const int tid = q8_tid();
+#pragma unroll 4
+    for (int i = 0; i < kRows / kStep; ++i) {
+        const int r = i * kStep + tid / W::kPieces, c = tid % W::kPieces;
+        const uint4 v = *reinterpret_cast<const uint4*>(tile8_at<W>(u0, u1, r, c));
+        if (r < rows) store(r, c, v);
+    }
 }
 
 template <int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void q8_gateup_kernel(Q8Args g) {
     typedef Tile8<MT, WAVES> W;
-    constexpr int H = W::kNi / 2, kCols = MT / 2, kPieces = kCols / 8;   // columns, 16-byte pieces of a row of results
+    constexpr int kCols = W::kCols;
     __shared__ __align__(16) char smem[W::kLds];
-    Q8Tile t;
-    if (!t.place(g, kCols)) return;
-    const int lane = threadIdx.x & 63;
-    Q8Rows<W::kLoads> a, b;
-    a.init(g.x, g.pitch, W::first(), [&](int r) {
-        r = t.row0 + (r < t.rows ? r : t.rows - 1);   // rows past the last one repeat it; what they give is not stored
-        return g.row_index ? g.row_index[r] : r;
-    });
-    b.init(W::wave() < WAVES / 2 ? g.w0 : g.w1, g.pitch, W::first(), [&](int r) {
-        const int n = t.n0 + (r & (kCols - 1));
-        return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
-    });
-    // the scales are fetched ahead of the loop
-    float xs[W::kMi], gs[H][4][4], us[H][4][4];
-#pragma unroll
-    for (int mi = 0; mi < W::kMi; ++mi) {
-        const int r = W::row(mi) + (lane & 31), row = t.row0 + (r < t.rows ? r : t.rows - 1);
-        xs[mi] = g.x_scale[g.row_index ? g.row_index[row] : row];
-    }
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int c = t.n0 + W::template col<true>(h) + 4 * (lane >> 5) + 8 * q;
-            q8_scales(g.s0 + (size_t)t.e * g.N, c, g.N, gs[h][q]);
-            q8_scales(g.s1 + (size_t)t.e * g.N, c, g.N, us[h][q]);
-        }
-    typename W::Acc acc;
-    tile8_product<W, true>(acc, a, b, g.pitch / 128, t.rows, smem);
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            gs[h][v / 4][v % 4] *= kLog2e;
-            us[h][v / 4][v % 4] *= 1.0f / kLog2e;
-        }
-    // results: rows of kCols columns, 16-byte pieces XOR-ed with the row
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-        const int c0 = W::template col<true>(h);
+    float xs[W::kMi], gs[4][4], us[4][4];
+    auto scales = [&](const Q8Tile& t) {
+        const int lane = q8_tid() & 63;
 #pragma unroll
         for (int mi = 0; mi < W::kMi; ++mi) {
-            const int r = W::row(mi) + (lane & 31);
-            uint2 o[4];
-            const float m = q8_activation(acc[mi][h], acc[mi][H + h], xs[mi], gs[h], us[h], o);
-            if (lane < 32 && r < t.rows) g.gmax[(size_t)(t.row0 + r) * (g.a_pitch / kQ8Group) + (t.n0 + c0) / kQ8Group] = m;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<uint2*>(smem + r * (2 * kCols) + (((c0 / 8 + q) ^ (r & (kPieces - 1))) << 4) + 8 * (lane >> 5)) =
-                    o[q];
+            const int r = W::row(mi) + (lane & 31), row = t.row0 + (r < t.rows ? r : t.rows - 1);
+            xs[mi] = g.x_scale[g.row_index ? g.row_index[row] : row];
         }
-    }
-    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < MT * kPieces / W::kThreads; ++i) {
-        const int r = i * (W::kThreads / kPieces) + threadIdx.x / kPieces, c = threadIdx.x % kPieces;
-        const uint4 v = *reinterpret_cast<const uint4*>(smem + r * (2 * kCols) + ((c ^ (r & (kPieces - 1))) << 4));
-        if (r < t.rows) *reinterpret_cast<uint4*>(g.a16 + (size_t)(t.row0 + r) * g.a_pitch + t.n0 + 8 * c) = v;
-    }
+        for (int q = 0; q < 4; ++q) {
+            const int c = t.n0 + W::col(0) + 4 * (lane >> 5) + 8 * q;
+            q8_scales(g.s0 + (size_t)t.e * g.N, c, g.N, gs[q]);
+            q8_scales(g.s1 + (size_t)t.e * g.N, c, g.N, us[q]);
+        }
+    };
+    tile8_run<W>(
+        g, kCols, smem,
+        [&](const Q8Tile& t, int r) {
+            r = t.row0 + (r < t.rows ? r : t.rows - 1);   // rows past the last one repeat it; what they give is not stored
+            return g.row_index ? g.row_index[r] : r;
+        },
+        [&](const Q8Tile& t, Q8Rows<W::kLoads>& b) {
+            b.init(W::wave() < WAVES / 2 ? g.w0 : g.w1, g.pitch, W::first(), [&](int r) {
+                const int n = t.n0 + (r & (kCols - 1));
+                return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
+            });
+        },
+        [&](const Q8Tile& t) {
+            if (!W::kRoll) scales(t);   // ahead of the loop, where the registers allow it
+        },
+        [&](const Q8Tile& t, typename W::Acc& acc, char* u0, char* u1) {
+            if (W::kRoll) scales(t);
+            const int lane = q8_tid() & 63;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                gs[v / 4][v % 4] *= kLog2e;
+                us[v / 4][v % 4] *= 1.0f / kLog2e;
+            }
+            const int c0 = W::col(0);
+#pragma unroll
+            for (int mi = 0; mi < W::kMi; ++mi) {
+                const int r = W::row(mi) + (lane & 31);
+                uint2 o[4];
+                const float m = q8_activation(acc[mi][0], acc[mi][1], xs[mi], gs, us, o);
+                if (lane < 32 && r < t.rows) g.gmax[(size_t)(t.row0 + r) * (g.a_pitch / kQ8Group) + (t.n0 + c0) / kQ8Group] = m;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(tile8_at<W>(u0, u1, r, c0 / 8 + q) + 8 * (lane >> 5)) = o[q];
+            }
+            q8_lds_barrier();
+            tile8_store<W>(u0, u1, t.rows, [&](int r, int c, const uint4& v) {
+                *reinterpret_cast<uint4*>(g.a16 + (size_t)(t.row0 + r) * g.a_pitch + t.n0 + 8 * c) = v;
+            });
+            if (W::kRoll) q8_lds_barrier();
+        });
 }
 
 template <int MT, int WAVES, typename T>
 __global__ __launch_bounds__(64 * WAVES, 2) void q8_down_kernel(Q8Args g) {
     typedef Tile8<MT, WAVES> W;
-    constexpr int kPieces = MT / 8;
     __shared__ __align__(16) char smem[W::kLds];
-    Q8Tile t;
-    if (!t.place(g, MT)) return;
-    const int lane = threadIdx.x & 63;
-    Q8Rows<W::kLoads> a, b;
-    a.init(g.x, g.pitch, W::first(), [&](int r) { return t.row0 + (r < t.rows ? r : t.rows - 1); });
-    b.init(g.w0, g.pitch, W::first(), [&](int r) {
-        const int n = t.n0 + r;
-        return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
-    });
-    float as[W::kMi];   // fetched ahead of the loop
+    float as[W::kMi];
+    auto scales = [&](const Q8Tile& t) {
+        const int lane = q8_tid() & 63;
 #pragma unroll
-    for (int mi = 0; mi < W::kMi; ++mi) {
-        const int r = W::row(mi) + (lane & 31);
-        as[mi] = g.x_scale[t.row0 + (r < t.rows ? r : t.rows - 1)];
-    }
-    typename W::Acc acc;
-    tile8_product<W, false>(acc, a, b, g.pitch / 128, t.rows, smem);
-#pragma unroll
-    for (int ni = 0; ni < W::kNi; ++ni)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int col = W::template col<false>(ni) + 8 * q + 4 * (lane >> 5);
-            float s[4];
-            q8_scales(g.s0 + (size_t)t.e * g.N, t.n0 + col, g.N, s);
-#pragma unroll
-            for (int mi = 0; mi < W::kMi; ++mi) {
-                const int r = W::row(mi) + (lane & 31);
-                float o[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = (float)acc[mi][ni][4 * q + i] * (as[mi] * s[i]);
-                if (sizeof(T) == 4) {
-                    if (r < t.rows) q8_store4((float*)g.y + (size_t)(t.row0 + r) * g.N, t.n0 + col, g.N, o);
-                } else {   // rows of MT columns, 16-byte pieces XOR-ed with the row
-                    *reinterpret_cast<uint2*>(smem + r * (2 * MT) + (((col >> 3) ^ (r & (kPieces - 1))) << 4) + 8 * (lane >> 5)) =
-                        make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
-                }
-            }
+        for (int mi = 0; mi < W::kMi; ++mi) {
+            const int r = W::row(mi) + (lane & 31);
+            as[mi] = g.x_scale[t.row0 + (r < t.rows ? r : t.rows - 1)];
         }
-    if (sizeof(T) == 4) return;
-    __syncthreads();
-#pragma unroll 4
-    for (int i = 0; i < MT * kPieces / W::kThreads; ++i) {
-        const int r = i * (W::kThreads / kPieces) + threadIdx.x / kPieces, c = threadIdx.x % kPieces;
-        const uint4 v = *reinterpret_cast<const uint4*>(smem + r * (2 * MT) + ((c ^ (r & (kPieces - 1))) << 4));
-        if (r < t.rows) q8_store8((bf16_t*)g.y + (size_t)(t.row0 + r) * g.N, t.n0 + 8 * c, g.N, v);
-    }
+    };
+    tile8_run<W>(
+        g, MT, smem, [&](const Q8Tile& t, int r) { return t.row0 + (r < t.rows ? r : t.rows - 1); },
+        [&](const Q8Tile& t, Q8Rows<W::kLoads>& b) {
+            b.init(g.w0, g.pitch, W::first(), [&](int r) {
+                const int n = t.n0 + r;
+                return (size_t)t.e * g.N + (n < g.N ? n : g.N - 1);
+            });
+        },
+        [&](const Q8Tile& t) {
+            if (!W::kRoll) scales(t);
+        },
+        [&](const Q8Tile& t, typename W::Acc& acc, char* u0, char* u1) {
+            if (W::kRoll) scales(t);
+            const int lane = q8_tid() & 63;
+#pragma unroll
+            for (int ni = 0; ni < W::kNi; ++ni) {   // MT / 2 columns of all waves
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = W::wn() * 32 + 8 * q + 4 * (lane >> 5), col = t.n0 + ni * W::kCols + c;
+                    float s[4];
+                    q8_scales(g.s0 + (size_t)t.e * g.N, col, g.N, s);
+#pragma unroll
+                    for (int mi = 0; mi < W::kMi; ++mi) {
+                        const int r = W::row(mi) + (lane & 31);
+                        float o[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] = (float)acc[mi][ni][4 * q + i] * (as[mi] * s[i]);
+                        if (sizeof(T) == 4) {
+                            if (r < t.rows) q8_store4((float*)g.y + (size_t)(t.row0 + r) * g.N, col, g.N, o);
+                        } else {
+                            *reinterpret_cast<uint2*>(tile8_at<W>(u0, u1, r, c / 8) + 8 * (lane >> 5)) =
+                                make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+                        }
+                    }
+                }
+                if (sizeof(T) == 4) continue;
+                q8_lds_barrier();
+                tile8_store<W>(u0, u1, t.rows, [&](int r, int c, const uint4& v) {
+                    q8_store8((bf16_t*)g.y + (size_t)(t.row0 + r) * g.N, t.n0 + ni * W::kCols + 8 * c, g.N, v);
+                });
+                if (W::kRoll || ni + 1 < W::kNi) q8_lds_barrier();
+            }
+        });
 }
+
+// blocks of the persistent kernels: one per CU
+constexpr long kQ8RollBlocks = 256;
 
 template <int MT, int WAVES>
 int launch_q8_gateup(const Q8Args& a, int max_tiles, hipStream_t s) {
-    const long blocks = q8_blocks(a.N, MT / 2, max_tiles);
+    typedef Tile8<MT, WAVES> W;
+    long blocks = q8_blocks(a.N, MT / 2, max_tiles);
+    if (W::kRoll && blocks > kQ8RollBlocks) blocks = kQ8RollBlocks;
     XMOE_LAUNCH(K_Q8_GATEUP, s,
                 hipLaunchKernelGGL((q8_gateup_kernel<MT, WAVES>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, s, a));
     return XMOE_OK;
 }
 template <int MT, int WAVES>
 int launch_q8_down(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
-    const dim3 grid((unsigned)q8_blocks(a.N, MT, max_tiles)), block(64 * WAVES);
+    typedef Tile8<MT, WAVES> W;
+    long blocks = q8_blocks(a.N, MT, max_tiles);
+    if (W::kRoll && blocks > kQ8RollBlocks) blocks = kQ8RollBlocks;
+    const dim3 grid((unsigned)blocks), block(64 * WAVES);
     if (dt == XMOE_F32)
         XMOE_LAUNCH(K_Q8_DOWN, s, hipLaunchKernelGGL((q8_down_kernel<MT, WAVES, float>), grid, block, 0, s, a));
     else
@@ -534,7 +627,7 @@ __global__ __launch_bounds__(256, 2) void q8_gateup_few_kernel(Q8Args g) {
     typedef Few8<2> F;
     __shared__ __align__(16) char smem[2 * F::kStage];
     Q8Tile t;
-    if (!t.place(g, 64)) return;
+    if (!t.place(g, 64, 1, blockIdx.x)) return;
     const int lane = threadIdx.x & 63, wave = F::wave(), half = lane >> 5;
     F p;
     p.w.init(wave < 2 ? g.w0 : g.w1, g.pitch, wave * 32, [&](int c) {
@@ -572,7 +665,7 @@ __global__ __launch_bounds__(256, 2) void q8_down_few_kernel(Q8Args g) {
     typedef Few8<1> F;
     __shared__ __align__(16) char smem[2 * F::kStage];
     Q8Tile t;
-    if (!t.place(g, 64)) return;
+    if (!t.place(g, 64, 1, blockIdx.x)) return;
     const int lane = threadIdx.x & 63, wave = F::wave();
     F p;
     p.w.init(g.w0, g.pitch, wave * 16, [&](int c) {
@@ -696,14 +789,23 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restri
 
 
 // Rows of a tile, by the mean load.  Measured (MI355X, all launches together, us, 256 | 128 | 32):
-//     mean rows                           1 - 2         8          16         62        124       248       500       1000
-//     64 experts + 2, d 2048, f 1408    122|99|88   177|146|131    - |152|142  197|177   236|200   281|290   479|490   834|885
-//     (32-row tiles at 31 and 47 mean rows: 155 for 156, 190 for 171; 8 experts, f 14336, 32 mean rows: 393 for 341)
-//     8 experts, d 2048, f 1408              (4) - |44|43           - |44|42    62|44     70|50     75|60     84|92   239|237 (2048)
-//     256 experts, d 2048, f 512        - |185|171       -         - |218|205  292|244   346|322   497|485
-//     64 experts, d 2048, Zipf load                                            186|171 (96)  260|253 (192)  431|407 (384)
-//     32 experts + 1, d 4096, f 1024                                           206|184 (155)  245|262 (310)  406|426 (621)
-int q8_tile_rows(int B, int E) { return B <= 16ll * E ? 32 : B <= 256ll * E ? 128 : 256; }
+//     mean rows                           1 - 2        8           16         62        124       186       248      364      496
+//     64 experts + 2, d 2048, f 1408    122|99|88  177|149|131   - |152|142  189|181   224|208   254|295   266|309  399|454  433|546
+//     8 experts, d 2048, f 1408                        |44|43         |44|42    62|44     70|50                75|63             84|96
+//     8 experts, d 4096, f 14336                                                        448|462             581|704            939| -
+//     256 experts, d 2048, f 512                                              264|256                       432|537
+//     24 experts, d 1000, f 712, Zipf                                                             62|63     70|70
+//     32 experts + 1, d 4096, f 1024                                                    199|186 (155)       233|275 (310)
+//     16 experts + 1, d 7168, f 2048                                                              300|287
+// (32-row tiles at 31 and 47 mean rows of 64 experts + 2: 155 for 128 rows' 156, 190 for 171.)  Up to 384 rows the larger tile
+// also has to come out at one tile for every CU; and K has two units or more, as the next tile's first are requested with
+// this one's last.
+int q8_tile_rows(int B, int E, int d, int f) {
+    if (B <= 16ll * E) return 32;
+    const long tiles = ((long)B / 256 + E) * ((f + 127) / 128);
+    if (B <= 160ll * E || (B <= 384ll * E && tiles < kQ8RollBlocks)) return 128;
+    return q8_pitch(d) < 256 || q8_pitch(f) < 256 ? 128 : 256;
+}
 
 }  // namespace
 }  // namespace xmoe
@@ -753,15 +855,15 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
     p += align_up((size_t)B * fp, 256);
     float* as = (float*)p;
     hipStream_t s = (hipStream_t)stream;
-    const int tile_rows = q8_tile_rows(B, E), max_tiles = ffn_max_tiles(B, E, tile_rows);
+    const int tile_rows = q8_tile_rows(B, E, d, f), max_tiles = ffn_max_tiles(B, E, tile_rows);
     // a grid has fewer than 2^32 threads: tiles of 64 columns and 256 threads are the most
     if (q8_blocks(f > d ? f : d, 64, max_tiles) * 256 >= (1l << 32)) return XMOE_ERR_UNSUPPORTED;
     int st = launch_tile_map(expert_offsets, E, tile_rows, max_tiles, map, map + ffn_q8_sched_offset(B, E), false, s);
     if (st != XMOE_OK) return st;
     const Q8Args up = {(const int8_t*)xq, x_scale, row_index, expert_offsets, map, (const int8_t*)wgq, (const int8_t*)wuq,
-                       g_scale, u_scale, dp, f, tile_rows, a16, gmax, fp, nullptr};
+                       g_scale, u_scale, dp, f, tile_rows, kQ8RowTiles, a16, gmax, fp, nullptr};
     const Q8Args down = {aq, as, nullptr, expert_offsets, map, (const int8_t*)wdq, nullptr, d_scale, nullptr, fp, d, tile_rows,
-                         nullptr, nullptr, 0, y};
+                         kQ8RowTiles, nullptr, nullptr, 0, y};
     st = tile_rows == 256   ? launch_q8_gateup<256, 8>(up, max_tiles, s)
          : tile_rows == 128 ? launch_q8_gateup<128, 4>(up, max_tiles, s)
                             : launch_q8_gateup_few(up, max_tiles, s);

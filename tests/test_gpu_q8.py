@@ -15,15 +15,16 @@ from gpu_util import launched
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 NEAR = 127 * (168 * U + 2.0 ** -16)
-ROWS = {      # mean loads up to 16, up to 256 and above: the three tile sizes
+ROWS = {      # mean loads up to 16, up to 160 or 384 and above: the three tile sizes
     "edges": [0, 1, 255, 256, 257, 0, 31],
     "few": [1, 0, 2, 33, 0, 64, 65] + [0] * 8,
     "middle": [1, 0, 2, 33, 0, 64, 65],
     "one long": [0, 900, 3],
     "even": [300, 257, 290],
     "single": [1],
+    "long": [1300, 0, 1100, 257, 1],
 }
-KERNELS = {"edges": 128, "few": 32, "middle": 128, "one long": 256, "even": 256, "single": 32}
+KERNELS = {"edges": 128, "few": 32, "middle": 128, "one long": 128, "even": 128, "single": 32, "long": 256}
 WIDTHS = [(1, 1), (64, 64), (130, 200), (257, 96), (1000, 712), (384, 1409)]   # d, f
 
 
@@ -47,6 +48,15 @@ def make(rows, d, f, gathered, seed=0):
     w = [oracle.quantize_rows(0.05 * g.standard_normal(s)) for s in ((E, f, d), (E, f, d), (E, d, f))]
     return dict(x=x.astype(np.int8), xs=xs.astype(np.float32), index=index, off=off,
                 w=[a.astype(np.int8) for a, _ in w], ws=[s.astype(np.float32) for _, s in w], B=B, E=E, d=d, f=f)
+
+
+def tile_rows(c):
+    B, E, d, f = c["B"], c["E"], c["d"], c["f"]
+    if B <= 16 * E:
+        return 32
+    if B <= 160 * E or (B <= 384 * E and (B // 256 + E) * -(-f // 128) < 256):
+        return 128
+    return 256 if min(pitch(d), pitch(f)) >= 256 else 128
 
 
 def call(m, c, dt, B=None, fill=7.0):
@@ -87,7 +97,18 @@ def check(c, got, dt):
 def test_against_the_oracle(rows, d, f, gathered, dt):
     import paper_2508_13337_amd as m
     c = make(ROWS[rows], d, f, gathered)
-    assert (32 if c["B"] <= 16 * c["E"] else 128 if c["B"] <= 256 * c["E"] else 256) == KERNELS[rows]
+    assert tile_rows(c) == (128 if rows == "long" and min(d, f) <= 128 else KERNELS[rows])
+    check(c, call(m, c, dt), dt)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,f,gathered", [(200, 2700, True), (5000, 200, False), (1700, 1900, True)])
+def test_more_tiles_than_blocks(d, f, gathered, dt):
+    """256-row tiles, several of them to a block: in the first product, in the second, in both."""
+    import paper_2508_13337_amd as m
+    c = make([2000, 700, 1, 0, 3100, 513], d, f, gathered)
+    tiles = sum(-(-n // 256) for n in (2000, 700, 1, 0, 3100, 513))
+    assert tile_rows(c) == 256 and max(tiles * -(-f // 128), tiles * -(-d // 256)) > 256
     check(c, call(m, c, dt), dt)
 
 
