@@ -173,8 +173,7 @@ struct Q8Args {
 };
 
 // Row tiles that go through the column tiles together.  The 32 CUs of an XCD then read 4 + 8 operand tiles at a time, not 1 + 32
-// (d 4096, f 14336, 8 experts with 512 rows each: 997 us, in twos 952, in fours 939, in eights 936; d 2048, f 1408, 66 with 500:
-// 464, 431, 427, 424).
+// (d 4096, f 14336, 8 experts with 512 rows each: 990 us, in fours 930; 33 experts, f 1024, 1241 mean rows: 655 and 637).
 constexpr int kQ8RowTiles = 4;
 // Tile L: row tiles x column tiles, in groups of `group` row tiles (those of a column tile, then the next column tile), dealt to
 // the XCDs in eight runs of equal length (workgroup L goes to XCD L % 8): tiles in flight together share their weights
@@ -203,9 +202,9 @@ long q8_blocks(int N, int cols, int max_tiles) { return ((long)max_tiles * ((N +
 // Tiles of MT x MT (gate/up: the same MT / 2 columns of both).  Units A(0) B(0) A(1) B(1) .. of MT rows x 128 k run through
 // five slots, two to three of them on their way.
 //   256: 8 waves (2 x 4) of 128 x 64 each, 160 KiB, one block per CU: the most products per byte of LDS.  A block takes tile
-//        after tile, and the units of the next one follow those of this one without a pause (against a block per tile: down
-//        264 us -> 247, gate/up 487 -> 481, with the order of the tiles 465; 66 experts, d 2048, f 1408, 993 mean rows: 1.63
-//        POP/s of the 2.08 of a large library product.  LDS reads and MFMA both take about half of the loop's time.)
+//        after tile, and the units of the next one follow those of this one without a pause (66 experts, d 2048, f 1408, 993
+//        mean rows: a block per tile 463 us for gate/up, 254 for down, this way 457 and 244: 1.65 POP/s, where a large library
+//        product has 2.08.  A unit pass takes the LDS reads and the matrix cores about 1.1 us each, and both together 2.2.)
 //   128: 4 waves (2 x 2) of 64 x 64 each, 80 KiB, two blocks per CU: where the weights' bytes are the bound, or 256 rows few
 // =========================================================================================================
 template <int MT, int WAVES>
@@ -789,14 +788,14 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restri
 
 
 // Rows of a tile, by the mean load.  Measured (MI355X, all launches together, us, 256 | 128 | 32):
-//     mean rows                           1 - 2        8           16         62        124       186       248      364      496
-//     64 experts + 2, d 2048, f 1408    122|99|88  177|149|131   - |152|142  189|181   224|208   254|295   266|309  399|454  433|546
-//     8 experts, d 2048, f 1408                        |44|43         |44|42    62|44     70|50                75|63             84|96
-//     8 experts, d 4096, f 14336                                                        448|462             581|704            939| -
-//     256 experts, d 2048, f 512                                              264|256                       432|537
-//     24 experts, d 1000, f 712, Zipf                                                             62|63     70|70
-//     32 experts + 1, d 4096, f 1024                                                    199|186 (155)       233|275 (310)
-//     16 experts + 1, d 7168, f 2048                                                              300|287
+//     mean rows                         1 - 2       8          16          62       124      155      186      248      496
+//     64 experts + 2, d 2048, f 1408  122|99|88  177|149|131  174|153|142  190|180  229|205  240|232  260|288  270|302  426|533
+//     8 experts, d 2048, f 1408                                                                                74|60    83|95
+//     8 experts, d 4096, f 14336                                                    440|466                   582|703  939| -
+//     256 experts, d 2048, f 512                                          266|247                             423|518
+//     24 experts, d 1000, f 712, Zipf                                                                60|55     68|64
+//     32 experts + 1, d 4096, f 1024                                                         201|189          233|272 (310)
+//     16 experts + 1, d 7168, f 2048                                                                302|292
 // (32-row tiles at 31 and 47 mean rows of 64 experts + 2: 155 for 128 rows' 156, 190 for 171.)  Up to 384 rows the larger tile
 // also has to come out at one tile for every CU; and K has two units or more, as the next tile's first are requested with
 // this one's last.
