@@ -53,11 +53,14 @@ def dtype_code(dt: torch.dtype) -> int:
     raise TypeError(f"xmoe supports float32 and bfloat16 storage, not {dt}")
 
 
-def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
+def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor", dev=None):
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
+    if dev is None or dev < 0:   # dev: the device that the call's tensors share (-1: host memory)
+        if not t.is_cuda:
+            raise ValueError(f"{name} must live on the GPU")
+    elif t.get_device() != dev:
+        raise ValueError(f"{name} must live on the GPU of the other tensors, {dev}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if dtype is not None and t.dtype != dtype:
@@ -65,9 +68,12 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
     return t.data_ptr()   # an int: the argument types make it a pointer, without an object per tensor
 
 
-def _stream():
+def _stream(dev=None):
     # the raw handle, without a torch.cuda.Stream object per call
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    current = torch.cuda.current_device()
+    if dev is not None and dev != current:
+        raise ValueError(f"the tensors live on GPU {dev}, the current device is {current}")
+    return torch._C._cuda_getCurrentRawStream(current)
 
 
 def xmoe_version() -> str:
@@ -391,10 +397,12 @@ def xmoe_add_rmsnorm(x, residual, gain, eps: float, h, y=None, q=None, q_scale=N
     assert (h is None or h.shape == x.shape) and (y is None or y.shape == x.shape)
     assert q is None or (q.shape[0] == T and q.shape[1] == xmoe_q8_pitch(d) and q.dim() == 2)
     assert (q_scale is None or q_scale.numel() == T) and (rstd is None or rstd.numel() == T)
-    _check(lib().xmoe_add_rmsnorm(_ptr(x, None, "x"), _ptr(residual, dt, "residual"), _ptr(gain, dt, "gain"), T, d,
-                                  float(eps), dtype_code(dt), _ptr(h, dt, "h"), _ptr(y, dt, "y"), _ptr(q, torch.int8, "q"),
-                                  _ptr(q_scale, torch.float32, "q_scale"), _ptr(rstd, torch.float32, "rstd"), _stream()),
-           "xmoe_add_rmsnorm")
+    dev = x.get_device()
+    _check(lib().xmoe_add_rmsnorm(
+        _ptr(x, None, "x", dev), _ptr(residual, dt, "residual", dev), _ptr(gain, dt, "gain", dev), T, d, float(eps),
+        dtype_code(dt), _ptr(h, dt, "h", dev), _ptr(y, dt, "y", dev), _ptr(q, torch.int8, "q", dev),
+        _ptr(q_scale, torch.float32, "q_scale", dev), _ptr(rstd, torch.float32, "rstd", dev),
+        _stream(dev)), "xmoe_add_rmsnorm")
 
 
 def xmoe_add_rmsnorm_bwd(dy, dh, h, gain, rstd, dx, dgain, ws) -> None:
@@ -403,18 +411,22 @@ def xmoe_add_rmsnorm_bwd(dy, dh, h, gain, rstd, dx, dgain, ws) -> None:
     dt = h.dtype
     assert tuple(dy.shape) == (T, d) and tuple(dx.shape) == (T, d) and (dh is None or tuple(dh.shape) == (T, d))
     assert gain.numel() == d and dgain.numel() == d and rstd.numel() == T
-    _check(lib().xmoe_add_rmsnorm_bwd(_ptr(dy, dt, "dy"), _ptr(dh, dt, "dh"), _ptr(h, None, "h"), _ptr(gain, dt, "gain"),
-                                      _ptr(rstd, torch.float32, "rstd"), T, d, dtype_code(dt), _ptr(dx, dt, "dx"),
-                                      _ptr(dgain, dt, "dgain"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
-           "xmoe_add_rmsnorm_bwd")
+    dev = h.get_device()
+    _check(lib().xmoe_add_rmsnorm_bwd(
+        _ptr(dy, dt, "dy", dev), _ptr(dh, dt, "dh", dev), _ptr(h, None, "h", dev), _ptr(gain, dt, "gain", dev),
+        _ptr(rstd, torch.float32, "rstd", dev), T, d, dtype_code(dt), _ptr(dx, dt, "dx", dev),
+        _ptr(dgain, dt, "dgain", dev), _ptr(ws, torch.uint8, "ws", dev), ws.numel(),
+        _stream(dev)), "xmoe_add_rmsnorm_bwd")
 
 
 def xmoe_quantize_weights(w, wq, scale) -> None:
     """w [E, K, N] -> wq [E, N, xmoe_q8_pitch(K)] int8 and scale [E, N]: what xmoe_expert_ffn_q8_fwd takes."""
     E, K, N = w.shape
     assert tuple(wq.shape) == (E, N, xmoe_q8_pitch(K)) and tuple(scale.shape) == (E, N)
-    _check(lib().xmoe_quantize_weights(_ptr(w, None, "w"), E, K, N, dtype_code(w.dtype), _ptr(wq, torch.int8, "wq"),
-                                       _ptr(scale, torch.float32, "scale"), _stream()), "xmoe_quantize_weights")
+    dev = w.get_device()
+    _check(lib().xmoe_quantize_weights(
+        _ptr(w, None, "w", dev), E, K, N, dtype_code(w.dtype), _ptr(wq, torch.int8, "wq", dev),
+        _ptr(scale, torch.float32, "scale", dev), _stream(dev)), "xmoe_quantize_weights")
 
 
 def xmoe_expert_ffn_q8_fwd(xq, x_scale, expert_offsets, wgq, g_scale, wuq, u_scale, wdq, d_scale, y, ws,
@@ -429,12 +441,13 @@ def xmoe_expert_ffn_q8_fwd(xq, x_scale, expert_offsets, wgq, g_scale, wuq, u_sca
     assert tuple(wgq.shape) == (E, f, dp) and wuq.shape == wgq.shape and u_scale.shape == g_scale.shape
     assert tuple(wdq.shape) == (E, d, fp) and tuple(d_scale.shape) == (E, d)
     i8, f32, i32 = torch.int8, torch.float32, torch.int32
+    dev = y.get_device()
     _check(lib().xmoe_expert_ffn_q8_fwd(
-        _ptr(xq, i8, "xq"), _ptr(x_scale, f32, "x_scale"), _ptr(row_index, i32, "row_index"),
-        _ptr(expert_offsets, i32, "expert_offsets"), B, E, d, f, _ptr(wgq, i8, "wgq"), _ptr(g_scale, f32, "g_scale"),
-        _ptr(wuq, i8, "wuq"), _ptr(u_scale, f32, "u_scale"), _ptr(wdq, i8, "wdq"), _ptr(d_scale, f32, "d_scale"),
-        _ptr(y, None, "y"), dtype_code(y.dtype), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
-        "xmoe_expert_ffn_q8_fwd")
+        _ptr(xq, i8, "xq", dev), _ptr(x_scale, f32, "x_scale", dev), _ptr(row_index, i32, "row_index", dev),
+        _ptr(expert_offsets, i32, "expert_offsets", dev), B, E, d, f, _ptr(wgq, i8, "wgq", dev),
+        _ptr(g_scale, f32, "g_scale", dev), _ptr(wuq, i8, "wuq", dev), _ptr(u_scale, f32, "u_scale", dev),
+        _ptr(wdq, i8, "wdq", dev), _ptr(d_scale, f32, "d_scale", dev), _ptr(y, None, "y", dev), dtype_code(y.dtype),
+        _ptr(ws, torch.uint8, "ws", dev), ws.numel(), _stream(dev)), "xmoe_expert_ffn_q8_fwd")
 
 
 def xmoe_layer_few_fwd(x, w_router, bias, wg, wu, wd, addend, logits, topk_idx, topk_w, out, ws) -> None:
@@ -449,11 +462,13 @@ def xmoe_layer_few_fwd(x, w_router, bias, wg, wu, wd, addend, logits, topk_idx, 
     assert tuple(logits.shape) == (T, E) and topk_idx.shape[0] == T and topk_w.shape == topk_idx.shape
     assert out.shape == x.shape
     f32 = torch.float32
+    dev = x.get_device()
     _check(lib().xmoe_layer_few_fwd(
-        _ptr(x, None, "x"), _ptr(w_router, dt, "w_router"), _ptr(bias, f32, "bias"), _ptr(wg, dt, "wg"), _ptr(wu, dt, "wu"),
-        _ptr(wd, dt, "wd"), _ptr(addend, dt, "addend"), T, d, E, Ea - E, k, f, dtype_code(dt), _ptr(logits, f32, "logits"),
-        _ptr(topk_idx, torch.int32, "topk_idx"), _ptr(topk_w, f32, "topk_w"), _ptr(out, dt, "out"),
-        _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()), "xmoe_layer_few_fwd")
+        _ptr(x, None, "x", dev), _ptr(w_router, dt, "w_router", dev), _ptr(bias, f32, "bias", dev),
+        _ptr(wg, dt, "wg", dev), _ptr(wu, dt, "wu", dev), _ptr(wd, dt, "wd", dev), _ptr(addend, dt, "addend", dev),
+        T, d, E, Ea - E, k, f, dtype_code(dt), _ptr(logits, f32, "logits", dev),
+        _ptr(topk_idx, torch.int32, "topk_idx", dev), _ptr(topk_w, f32, "topk_w", dev), _ptr(out, dt, "out", dev),
+        _ptr(ws, torch.uint8, "ws", dev), ws.numel(), _stream(dev)), "xmoe_layer_few_fwd")
 
 
 def xmoe_prof_enable(on: bool) -> None:
