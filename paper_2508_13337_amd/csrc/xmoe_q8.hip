@@ -204,7 +204,9 @@ long q8_blocks(int N, int cols, int max_tiles) { return ((long)max_tiles * ((N +
 //   256: 8 waves (2 x 4) of 128 x 64 each, 160 KiB, one block per CU: the most products per byte of LDS.  A block takes tile
 //        after tile, and the units of the next one follow those of this one without a pause (66 experts, d 2048, f 1408, 993
 //        mean rows: a block per tile 463 us for gate/up, 254 for down, this way 457 and 244: 1.65 POP/s, where a large library
-//        product has 2.08.  A unit pass takes the LDS reads and the matrix cores about 1.1 us each, and both together 2.2.)
+//        product has 2.08).  Matrix cores are busy 43 % of it: a pass reads 192 KiB of LDS and writes 64, as long at 128 bytes a
+//        clock as its matrix instructions take, and the two overlap in part only.  (Waves of higher priority in their matrix
+//        instructions: 1 to 2 % slower.)
 //   128: 4 waves (2 x 2) of 64 x 64 each, 80 KiB, two blocks per CU: where the weights' bytes are the bound, or 256 rows few
 // =========================================================================================================
 template <int MT, int WAVES>
@@ -528,9 +530,9 @@ int launch_q8_down(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
 // the second on its way while the first is multiplied, 40 KiB each for gate/up (two blocks per CU), 24 for down (three).
 // Waves 0, 1 and 2, 3 take half of a stage's k each, and their sums, which are integers, are added in LDS.  Tried: straight
 // from memory to registers, 32 bytes of 32 rows at a time (slower by a quarter, the loads' addresses take the L1 cache too
-// long); 128 columns for down (34 experts, d 2048, f 1408: 29 us for 23, too few blocks for an even load); 32 for gate/up (51
-// for 48); 64 rows (one block per CU: 95 for 76).  Measured, d 2048, f 1408, 37 of 66 experts with one or two rows each:
-// gate/up 44 us (4.8 TB/s), down 23 (4.6); all 66: 72 (5.3) and 39 (4.9).
+// long); 128 columns for down (37 experts, d 2048, f 1408: 30 us for 25, too few blocks for an even load); 32 for gate/up (48
+// for 45); 64 rows (one block per CU: 95 for 76).  Measured, d 2048, f 1408, 37 of 66 experts with one or two rows each:
+// gate/up 45 us (4.7 TB/s), down 25 (4.3); all 66: 72 (5.3) and 39 (4.9).
 // =========================================================================================================
 __device__ __align__(16) const uint32_t kQ8Zero[4] = {0u, 0u, 0u, 0u};
 
