@@ -171,9 +171,10 @@ class XMoELayer:
 def capture_step(layer, x: torch.Tensor, w: dict, dout: torch.Tensor, grads: dict, residual: Optional[torch.Tensor] = None,
                  dh: Optional[torch.Tensor] = None) -> "torch.cuda.CUDAGraph":
     """Records one forward + backward of `layer` (either class; residual, dh: for one with a norm) into a HIP graph and
-    returns it; `graph.replay()` then runs the step with one launch instead of two dozen.  The library's calls only enqueue kernels on the current
-    stream (no allocation, no synchronisation, no memset nodes: counters are cleared by kernels), so they can be
-    captured as they are.  All tensors are captured by address: refill x, dout and the weights in place."""
+    returns it; `graph.replay()` then runs the step with one launch instead of two dozen.  The library's calls only
+    enqueue kernels on the current stream (no allocation, no synchronisation, no memset nodes: counters are cleared by
+    kernels), so they can be captured as they are.  All tensors are captured by address: refill x, dout and the weights
+    in place."""
     more = {} if residual is None else {"residual": residual}
     more_bwd = {} if dh is None else {"dh": dh}
     side = torch.cuda.Stream()
