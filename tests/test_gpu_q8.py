@@ -112,6 +112,43 @@ def test_more_tiles_than_blocks(d, f, gathered, dt):
     check(c, call(m, c, dt), dt)
 
 
+@pytest.mark.parametrize("rows,d,f", [([3, 0, 20, 1], 384, 712), ([300, 20, 257, 0], 384, 712), ([1300, 900, 700], 320, 2700)])
+def test_two_calls_at_once_and_a_replayed_graph(rows, d, f):
+    """Of every tile size: two streams with buffers of their own, then both calls in one graph on one workspace."""
+    import paper_2508_13337_amd as m
+    cs = [make(rows, d, f, True, seed=s) for s in (1, 2)]
+    ws = [m.alloc_workspace(m.xmoe_workspace_bytes(m.WS_FFN_Q8_FWD, c["B"], d, c["E"], 1, f, m.XMOE_BF16)) for c in cs]
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    args = [[dev(a) for a in (padded(c["x"]), c["xs"], c["off"], padded(c["w"][0]), c["ws"][0], padded(c["w"][1]), c["ws"][1],
+                              padded(c["w"][2]), c["ws"][2])] for c in cs]
+    index = [dev(c["index"]) for c in cs]
+    y = [torch.empty((c["B"], d), dtype=torch.bfloat16, device="cuda") for c in cs]
+    run = lambda i, w: m.xmoe_expert_ffn_q8_fwd(*args[i], y[i], ws[w], row_index=index[i])
+    for i in (0, 1):
+        run(i, i)
+    want = [t.clone() for t in y]
+    for c, t in zip(cs, want):
+        check(c, t.cpu(), torch.bfloat16)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cs]
+    for turn in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                run(i, i)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, y))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(0, 0)
+        run(1, 0)
+    for turn in range(4):
+        for t in y:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, y)), turn
+
+
 def test_serving_shape():
     import paper_2508_13337_amd as m
     c = make([0, 40, 13, 600, 1, 300], 2048, 1408, True)
