@@ -404,7 +404,7 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
                            size_t ws_bytes, void* stream);
 
 /* A whole layer for a few tokens (a decoding step), forward only: xmoe_gate_logits, xmoe_route, the SwiGLU experts and
- * xmoe_combine in four launches (five with a router of more than 128 experts or 512 KiB), without index arrays:
+ * xmoe_combine in four launches (five with a router of more than 128 experts or 256 KiB), without index arrays:
  *   out[t,:] = sum_j topk_w[t,j] * FFN_e(x[t]) with e = topk_idx[t,j], + sum_s FFN_{E+s}(x[t]) (+ addend[t,:])
  * x [T,d], w_router [d,E], bias [E] float32 or NULL, wg, wu [E+E_s,d,f], wd [E+E_s,f,d] (the shared experts behind the routed
  * ones), addend [T,d] or NULL, all dt but bias.  Outputs: logits [T,E], topk_idx, topk_w [T,k] as xmoe_gate_logits and

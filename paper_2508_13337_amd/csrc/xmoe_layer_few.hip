@@ -6,13 +6,17 @@
 // routing goes through tables in memory: a token's choice is a few integers, and every block finds the active experts and
 // their tokens (a 32-bit mask per expert) in LDS by itself.
 //
-//   route   one block per token: logits in the fixed order of xmoe_gate_logits (a lane is one of the 64 partial sums), top-k.
-//   up      A = silu(x Wg) * (x Wu) of an active expert and 64 of its columns
-//   down    A Wd of an active expert and 128 columns, float32, one row for each (token, expert); the block that finishes a
-//           tile of columns last adds the tokens' rows up, in the order of the slots: the result does not depend on which.
+//   route   one block per token: logits in the fixed order of xmoe_gate_logits, top-k (large routers: that call and xmoe_route)
+//   up      A = silu(x Wg) * (x Wu) of an active expert and 64 or 128 of its columns
+//   down    A Wd of an active expert, 256 columns and a slab of f, float32, one row for each (token, expert) and slab
+//   sum     the tokens' rows, slabs and slots in order
 //
-// Two families of products: bf16 with widths that are multiples of 64 on the matrix cores (the ring of xmoe_few_tile.h),
-// everything else on the vector ALUs, where 16 groups of threads share a tile's K and read the weights straight to registers.
+// Two families of products: bf16 with widths that are multiples of 8 on the matrix cores, weights on a ring of direct-to-LDS
+// stages; everything else on the vector ALUs, where 16 groups of threads share a tile's K and read the weights straight to
+// registers.  d 2048, f 1408, 6 of 64 experts + 2, bf16: one token 45 us (11.8 + 19.5 + 10.4 + 4.1 and the gaps; 139 MB in up and
+// down at 4.6 TB/s), 16 tokens 189 (11.4 + 113 + 58 + 4.9; 5.2 TB/s).
+// Tried: a launch less, the last block of a column's down tiles adding the rows (a fence by every block: slower), and one
+// launch for all of it with a ticket per item (an atomic on one address takes 60 to 75 ns: 71 us for one token).
 #include "xmoe_ffn.h"
 #include "xmoe_route.h"
 
@@ -622,10 +626,14 @@ int launch_layer_route(const LayerArgs& a, hipStream_t s) {
     return XMOE_OK;
 }
 
-// A block per token reads the whole router: up to this many bytes of it
-constexpr size_t kRouteBytes = 512 << 10;
-// From this many tiles of 128 columns on, up takes them (rows of 256 bytes of either matrix) instead of 64
-constexpr long kWideTiles = 400;
+// A block per token reads the whole router through one CU: up to this many bytes of it.  The whole call, us, so | by
+// xmoe_gate_logits and xmoe_route: 256 KiB (d 2048, 64 experts) 1 token 27.8|28.9, 32 tokens 40.0|40.5; 512 KiB (d 2048, 128
+// experts) 33.8|29.2 and 55.9|51.3, (d 4096, 64) 41.8|41.4 and 72.4|73.4; 1 MiB 50.8|41.6.
+constexpr size_t kRouteBytes = 256 << 10;
+// From this many tiles of 128 columns on, up takes them (rows of 256 bytes of either matrix) instead of 64.  The whole call, us,
+// 128 | 64 columns, d 2048, f 1408: 88 tiles 55.8|48.9, 154 65.4|71.4, 286 98.4|97.6, 550 137.8|143.6, 726 189|185; d 4096, f 14336:
+// 224 tiles 149|162, 896 329|342; d 4096, f 1024: 264 tiles 134|149; d 1024, f 512: 64 tiles 28.0|24.0, 256 50.4|54.7.
+constexpr long kWideTiles = 128;
 
 }  // namespace
 }  // namespace xmoe
