@@ -96,7 +96,8 @@ __device__ __forceinline__ void q8_scales(const float* __restrict__ scale, int c
 }
 // A row's 32 columns of gate and up sums (this lane: 16 of them) -> 16-bit integers, packed in the order of the registers'
 // column quadruples, and the maximum of all 32.  gs: the gate columns' scales times log2 e, us: the up columns' divided by
-// it.  The row's scale is a factor of up that integers and maximum have in common: it goes to the maximum alone.
+// it.  The row's scale is a factor of up that integers and maximum have in common: its size goes to the maximum alone, its
+// sign to the integers.
 __device__ __forceinline__ float q8_activation(const q8_i32x16_t& g, const q8_i32x16_t& u, float xs,
                                                const float (&gs)[4][4], const float (&us)[4][4], uint2 (&out)[4]) {
     float a[16], m = 0.f;
@@ -107,7 +108,7 @@ __device__ __forceinline__ float q8_activation(const q8_i32x16_t& g, const q8_i3
         m = __builtin_elementwise_maximum(m, fabsf(a[v]));   // a NaN stays
     }
     m = __builtin_elementwise_maximum(m, __shfl_xor(m, 32, 64));
-    const float inv = m < kQ8Tiny ? 0.f : __builtin_amdgcn_rcpf(m);
+    const float inv = m < kQ8Tiny ? 0.f : copysignf(__builtin_amdgcn_rcpf(m), xs);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {   // to the nearest of 32767 steps to one, in one instruction for two
         uint32_t w[2];
