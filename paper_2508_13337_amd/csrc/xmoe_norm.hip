@@ -173,7 +173,8 @@ __global__ __launch_bounds__(norm_block(TPR)) void add_rmsnorm_kernel(const T* x
         // below 2^-120 the quotient would overflow: such a row counts as zero
         const float m = __uint_as_float(mx);
         const bool none = mx < 0x03800000u;
-        const float inv = none ? 0.f : 127.0f / m;
+        // a maximum that is no number: 0 keeps the zeros past d (and 127 / inf does)
+        const float inv = none || mx > 0x7f800000u ? 0.f : 127.0f / m;
         if (i0 == 0) q_scale[t] = none ? 0.f : m * r / 127.0f;
         int8_t* row = q + (size_t)t * pitch;
 #pragma unroll
