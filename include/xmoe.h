@@ -362,6 +362,7 @@ int xmoe_gate_logits_bwd(const void* x, const void* w_router, const float* dlogi
  * q_scale = 0).  The integers do not depend on the order of any sum.
  * The mean of the squares is a float32 sum: it has to stay finite.  A row that holds an infinity or a NaN gives NaN in
  * the affected y, and a q_scale that is not finite.
+ * A row's results do not depend on the call's other rows (dgain of the backward is a sum over them).
  * d <= XMOE_MAX_NORM_WIDTH, T < 2^22.
  */
 int xmoe_add_rmsnorm(const void* x, const void* residual, const void* gain, int T, int d, float eps, int dt, void* h,

@@ -11,7 +11,9 @@
 // thread t on the vectors t, t + TPR, ...  Rows whose width is no multiple of a vector are read and written by the same
 // vectors from addresses aligned to one element, and the last one element by element.
 // Sums are float32: of a thread's elements in ascending order, then by halving over the wave, then over the waves in
-// order; dgain over a block's rows in order, then over the blocks' partial rows.  Nothing depends on which block is first.
+// order; dgain over a block's rows in order, then over the blocks' partial rows.  Nothing depends on which block is first, and
+// a row's bits not on the number of rows, by which the threads of a row are chosen up to 256 vectors: 64 vectors are a sum of
+// their own whether one wave has all of them or four have 64 each.
 #include "xmoe_internal.h"
 #include "xmoe_sizes.h"
 
@@ -63,6 +65,11 @@ struct NormRow {
         if (N == 4) return __uint_as_float(w[j]);
         return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
     }
+    // from here on nothing is known of the words
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(w[j]));
+    }
     // the values rounded to the storage type
     __device__ __forceinline__ void round(const float (&f)[N]) {
 #pragma unroll
@@ -78,31 +85,57 @@ __device__ __forceinline__ bf16_t NormRow<bf16_t>::element(int j) const {
     return bf16_t{(uint16_t)(w[j / 2] >> (16 * (j & 1)))};
 }
 
-// the row's sum (and the largest of `mx`), the same in all of its TPR threads.  Every thread of the block calls it; the
+// Sums that a thread keeps of its NV vectors: of each where a wave has the row, so that 64 vectors are one sum as they are
+// where a wave has no more; else one.
+constexpr int norm_sums(int tpr, int nv) { return tpr == 64 ? nv : 1; }
+
+// The row's sum (and the largest of `mx`), the same in all of its TPR threads.  Every thread of the block calls it; the
 // LDS is free again for a call with another `part`.
-template <int TPR>
-__device__ __forceinline__ void norm_row_reduce(float& sum, uint32_t& mx, float* part_s, uint32_t* part_m) {
+// A wave's S sums are halved together: a lane hands over those that its partner keeps, until it has one, the lane's bits 5 and
+// 4 telling which; every sum's tree is that of S = 1.
+template <int TPR, int S>
+__device__ __forceinline__ float norm_row_reduce(const float (&sums)[S], uint32_t& mx, float* part_s, uint32_t* part_m) {
+    static_assert(S == 1 || S == 2 || S == 4, "a lane's bits 5 and 4");
+    float v[S];
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        sum += __shfl_xor(sum, off, 64);
-        const uint32_t o = (uint32_t)__shfl_xor((int)mx, off, 64);
-        mx = o > mx ? o : mx;
-    }
-    if (TPR > 64) {
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-            part_s[wave] = sum;
-            part_m[wave] = mx;
-        }
-        __syncthreads();
-        sum = 0.f;
-        mx = 0u;
+    for (int n = 0; n < S; ++n) v[n] = sums[n];
+    int off = 32;
 #pragma unroll
-        for (int w = 0; w < TPR / 64; ++w) {
-            sum += part_s[w];
-            mx = part_m[w] > mx ? part_m[w] : mx;
+    for (int s = S / 2; s >= 1; s /= 2, off /= 2) {
+        const bool upper = (threadIdx.x & off) != 0;
+#pragma unroll
+        for (int n = 0; n < s; ++n) {
+            const float keep = upper ? v[n + s] : v[n], give = upper ? v[n] : v[n + s];
+            v[n] = keep + __shfl_xor(give, off, 64);
         }
     }
+#pragma unroll
+    for (; off >= 1; off >>= 1) v[0] += __shfl_xor(v[0], off, 64);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        const uint32_t m = (uint32_t)__shfl_xor((int)mx, o, 64);
+        mx = m > mx ? m : mx;
+    }
+    float sum = 0.f;
+    if (TPR == 64) {
+#pragma unroll
+        for (int n = 0; n < S; ++n)
+            sum += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[0]), n * (64 / S)));
+        return sum;
+    }
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        part_s[wave] = v[0];
+        part_m[wave] = mx;
+    }
+    __syncthreads();
+    mx = 0u;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) {
+        sum += part_s[w];
+        mx = part_m[w] > mx ? part_m[w] : mx;
+    }
+    return sum;
 }
 
 constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
@@ -110,11 +143,9 @@ constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
 // q: rows of `pitch` bytes, zeros behind the first d.  h may be x or residual: a thread has read its elements of both
 // before it writes.
 template <typename T, int TPR, int NV>
-__global__ __launch_bounds__(norm_block(TPR)) void add_rmsnorm_kernel(const T* x, const T* residual,
-                                                                      const T* __restrict__ gain, int Tn, int d, float eps,
-                                                                      T* h, T* __restrict__ y, int8_t* __restrict__ q,
-                                                                      int pitch, float* __restrict__ q_scale,
-                                                                      float* __restrict__ rstd) {
+__global__ __launch_bounds__(norm_block(TPR)) void add_rmsnorm_kernel(
+    const T* x, const T* residual, const T* __restrict__ gain, int Tn, int d, float eps, T* h, T* __restrict__ y,
+    int8_t* __restrict__ q, int pitch, float* __restrict__ q_scale, float* __restrict__ rstd) {
     typedef NormRow<T> Row;
     constexpr int N = Row::N, RPB = norm_block(TPR) / TPR;
     __shared__ float part_s[norm_block(TPR) / 64];
@@ -144,18 +175,27 @@ __global__ __launch_bounds__(norm_block(TPR)) void add_rmsnorm_kernel(const T* x
         for (int n = 0; n < NV; ++n) v[n].store(h + at, i0 + n * TPR * N, d);
     }
     // the maximum of the bit patterns without the sign: as of the numbers, and a NaN is above them all
-    float sum = 0.f;
+    constexpr int S = norm_sums(TPR, NV);
+    float sums[S];
+#pragma unroll
+    for (int n = 0; n < S; ++n) sums[n] = 0.f;
     uint32_t mx = 0u;
 #pragma unroll
     for (int n = 0; n < NV; ++n)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const float a = v[n].at(j);
-            sum = fmaf(a, a, sum);
+            sums[n % S] = fmaf(a, a, sums[n % S]);
             const uint32_t b = __float_as_uint(a * g[n].at(j)) & 0x7fffffffu;
             mx = b > mx ? b : mx;
         }
-    norm_row_reduce<TPR>(sum, mx, part_s, part_m);
+    const float sum = norm_row_reduce<TPR>(sums, mx, part_s, part_m);
+    // the elements are widened again below: as floats, held over the sum, they would take twice the registers
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+        v[n].renew();
+        g[n].renew();
+    }
     const float r = 1.0f / sqrtf(sum / (float)d + eps);
     if (rstd && i0 == 0) rstd[t] = r;
     if (y) {
@@ -234,18 +274,20 @@ __global__ __launch_bounds__(norm_block(TPR)) void add_rmsnorm_bwd_kernel(const 
         constexpr bool kLate = TPR * NV > 2048;   // the widest rows: 128 registers do not hold all three at once
         if (!kLate) load_dh();
         const float r = rstd[t];
-        float sum = 0.f;
+        constexpr int S = norm_sums(TPR, NV);
+        float sums[S];
+#pragma unroll
+        for (int n = 0; n < S; ++n) sums[n] = 0.f;
         uint32_t none = 0u;
 #pragma unroll
         for (int n = 0; n < NV; ++n)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const float nrm = a[n].at(j) * r, v = b[n].at(j);
-                sum = fmaf(v * g[n].at(j), nrm, sum);
+                sums[n % S] = fmaf(v * g[n].at(j), nrm, sums[n % S]);
                 acc[n][j] = fmaf(v, nrm, acc[n][j]);
             }
-        norm_row_reduce<TPR>(sum, none, part_s[turn], part_m[turn]);
-        const float mean = sum / (float)d;
+        const float mean = norm_row_reduce<TPR>(sums, none, part_s[turn], part_m[turn]) / (float)d;
         if (kLate) load_dh();
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
