@@ -391,7 +391,7 @@ int xmoe_quantize_weights(const void* w, int E, int K, int N, int dt, void* wq, 
  *   G[r,n] = x_scale[r] g_scale[e,n] sum_k xq[r,k] wgq[e,n,k],  U likewise with wuq, u_scale;   A = silu(G) * U;
  *   aq[r,:], as[r] = A's row as 8-bit integers with one scale, as xmoe_add_rmsnorm makes them;
  *   Y[r,n] = as[r] d_scale[e,n] sum_k aq[r,k] wdq[e,n,k]
- * The sums over k are exact integers.  On its way to aq, A is held as 16-bit integers relative to the largest of 32 columns.
+ * The sums over k are exact integers; G, U and A are float32.
  * xq: int8 rows of xmoe_q8_pitch(d) bytes (xmoe_add_rmsnorm's q), x_scale float32, one for each; row_index, expert_offsets,
  * B, E as in xmoe_expert_ffn_fwd (with row_index, xq and x_scale are the tokens' and row i is row row_index[i] of both).
  * wgq, wuq [E,f,xmoe_q8_pitch(d)], wdq [E,d,xmoe_q8_pitch(f)] int8; g_scale, u_scale [E,f], d_scale [E,d] float32

@@ -8,10 +8,9 @@
 // 128 k is one cache line of each row, and widths that are no multiple of anything have no special case but the edge of an
 // output tile.
 //
-// A row's scale is known when all columns of A are.  The product therefore leaves A as 16-bit integers relative to the
-// maximum of every 32 columns (half a step: 2^-16 of that maximum, 1/500 of a step of the 8 bits that follow) with those
-// maxima in float32, and a pass over them (q8_rows_kernel) makes the 8-bit rows: the row's maximum is the largest of the 32-column
-// ones, so this pass reads A once, at half of float32's bytes.
+// A row's scale is known when all columns of A are.  The product therefore leaves A in float32 with the maximum of every 32
+// columns, and a pass over it (q8_rows_kernel) makes the 8-bit rows: the row's maximum is the largest of the 32-column ones, so
+// this pass reads A once.
 #include "xmoe_ffn.h"
 
 namespace xmoe {
@@ -20,9 +19,7 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) int q8_i32x4_t;
 typedef __attribute__((ext_vector_type(16))) int q8_i32x16_t;
 
-constexpr int kQ8Group = 32;       // columns of A that share a 16-bit scale
-constexpr float kQ8Tiny = 0x1p-112f;   // a maximum below counts as zero: 32767 / it would overflow
-constexpr uint32_t kQ8TinyBits = (127 - 112) << 23;
+constexpr int kQ8Group = 32;       // columns of A that share a maximum
 
 __device__ __forceinline__ void q8_load16(const int8_t* p, char* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
@@ -94,30 +91,23 @@ __device__ __forceinline__ void q8_scales(const float* __restrict__ scale, int c
         for (int i = 0; i < 4; ++i) s[i] = col + i < N ? scale[col + i] : 0.f;   // columns past N: zero
     }
 }
-// A row's 32 columns of gate and up sums (this lane: 16 of them) -> 16-bit integers, packed in the order of the registers'
-// column quadruples, and the maximum of all 32.  gs: the gate columns' scales times log2 e, us: the up columns' divided by
-// it.  The row's scale is a factor of up that integers and maximum have in common: its size goes to the maximum alone, its
-// sign to the integers.
+// A row's 32 columns of gate and up sums (this lane: 16 of them) -> A, four columns after the other at out, out + 8, ..; the
+// maximum of all 32.  gs: the gate columns' scales times log2 e, us: the up columns' divided by it.
 __device__ __forceinline__ float q8_activation(const q8_i32x16_t& g, const q8_i32x16_t& u, float xs,
-                                               const float (&gs)[4][4], const float (&us)[4][4], uint2 (&out)[4]) {
+                                               const float (&gs)[4][4], const float (&us)[4][4], float* out, bool store) {
     float a[16], m = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-        const float gv = (float)g[v] * xs * gs[v / 4][v % 4], uv = (float)u[v] * us[v / 4][v % 4];
+        const float gv = (float)g[v] * xs * gs[v / 4][v % 4], uv = (float)u[v] * xs * us[v / 4][v % 4];
         a[v] = gv * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-gv)) * uv;
         m = __builtin_elementwise_maximum(m, fabsf(a[v]));   // a NaN stays
     }
-    m = __builtin_elementwise_maximum(m, __shfl_xor(m, 32, 64));
-    const float inv = m < kQ8Tiny ? 0.f : copysignf(__builtin_amdgcn_rcpf(m), xs);
+    if (store) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {   // to the nearest of 32767 steps to one, in one instruction for two
-        uint32_t w[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_i16(a[4 * q + 2 * i] * inv, a[4 * q + 2 * i + 1] * inv));
-        out[q] = make_uint2(w[0], w[1]);
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<float4*>(out + 8 * q) = make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
     }
-    return m * fabsf(xs);
+    return __builtin_elementwise_maximum(m, __shfl_xor(m, 32, 64));
 }
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -167,7 +157,7 @@ struct Q8Args {
     const float *s0, *s1;       // [E, N]
     int pitch, N, tile_rows;    // tile_rows: the tile map's
     int group;                  // row tiles that go through the column tiles together
-    int16_t* a16;               // gate/up: [rows][a_pitch]
+    float* a32;                 // gate/up: [rows][a_pitch]
     float* gmax;                // [rows][a_pitch / 32]
     int a_pitch;
     void* y;                    // down: [rows][N]
@@ -416,7 +406,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q8_gateup_kernel(Q8Args g) {
         [&](const Q8Tile& t) {
             if (!W::kRoll) scales(t);   // ahead of the loop, where the registers allow it
         },
-        [&](const Q8Tile& t, typename W::Acc& acc, char* u0, char* u1) {
+        [&](const Q8Tile& t, typename W::Acc& acc, char*, char*) {
             if (W::kRoll) scales(t);
             const int lane = q8_tid() & 63;
 #pragma unroll
@@ -428,17 +418,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q8_gateup_kernel(Q8Args g) {
 #pragma unroll
             for (int mi = 0; mi < W::kMi; ++mi) {
                 const int r = W::row(mi) + (lane & 31);
-                uint2 o[4];
-                const float m = q8_activation(acc[mi][0], acc[mi][1], xs[mi], gs, us, o);
-                if (lane < 32 && r < t.rows) g.gmax[(size_t)(t.row0 + r) * (g.a_pitch / kQ8Group) + (t.n0 + c0) / kQ8Group] = m;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(tile8_at<W>(u0, u1, r, c0 / 8 + q) + 8 * (lane >> 5)) = o[q];
+                const size_t row = t.row0 + r;
+                // a wave writes whole cache lines of its rows, 32 bytes of each at a time
+                const float m = q8_activation(acc[mi][0], acc[mi][1], xs[mi], gs, us,
+                                              g.a32 + row * g.a_pitch + t.n0 + c0 + 4 * (lane >> 5), r < t.rows);
+                if (lane < 32 && r < t.rows) g.gmax[row * (g.a_pitch / kQ8Group) + (t.n0 + c0) / kQ8Group] = m;
             }
-            q8_lds_barrier();
-            tile8_store<W>(u0, u1, t.rows, [&](int r, int c, const uint4& v) {
-                *reinterpret_cast<uint4*>(g.a16 + (size_t)(t.row0 + r) * g.a_pitch + t.n0 + 8 * c) = v;
-            });
-            if (W::kRoll) q8_lds_barrier();
         });
 }
 
@@ -654,12 +639,9 @@ __global__ __launch_bounds__(256, 2) void q8_gateup_few_kernel(Q8Args g) {
         gs[v / 4][v % 4] *= kLog2e;
         us[v / 4][v % 4] *= 1.0f / kLog2e;
     }
-    uint2 o[4];
-    const float m = q8_activation(F::sum(smem, 0, wave & 1), F::sum(smem, 1, wave & 1), xs, gs, us, o);
-    if (r >= t.rows) return;
-    if (half == 0) g.gmax[(size_t)row * (g.a_pitch / kQ8Group) + c0 / kQ8Group] = m;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint2*>(g.a16 + (size_t)row * g.a_pitch + c0 + 4 * half + 8 * q) = o[q];
+    const float m = q8_activation(F::sum(smem, 0, wave & 1), F::sum(smem, 1, wave & 1), xs, gs, us,
+                                  g.a32 + (size_t)row * g.a_pitch + c0 + 4 * half, r < t.rows);
+    if (half == 0 && r < t.rows) g.gmax[(size_t)row * (g.a_pitch / kQ8Group) + c0 / kQ8Group] = m;
 }
 
 template <typename T>
@@ -708,7 +690,7 @@ int launch_q8_down_few(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
 // =========================================================================================================
 // A's 8-bit rows: one wave per row.  HBM-bound.
 // =========================================================================================================
-__global__ __launch_bounds__(256) void q8_rows_kernel(const int16_t* __restrict__ a16, const float* __restrict__ gmax,
+__global__ __launch_bounds__(256) void q8_rows_kernel(const float* __restrict__ a32, const float* __restrict__ gmax,
                                                       const int32_t* __restrict__ off, int E, int f, int pitch,
                                                       int8_t* __restrict__ aq, float* __restrict__ as) {
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -725,22 +707,21 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const int16_t* __restrict_
         const uint32_t o = (uint32_t)__shfl_xor((int)mx, w, 64);
         mx = o > mx ? o : mx;
     }
-    const float m = __uint_as_float(mx), inv = mx < kQ8TinyBits ? 0.f : 127.f / m;
-    if (lane == 0) as[row] = mx < kQ8TinyBits ? 0.f : m / 127.f;
-    const int16_t* src = a16 + (size_t)row * pitch;
+    // as xmoe_add_rmsnorm: below 2^-120 the quotient would overflow, such a row counts as zero
+    const bool none = mx < 0x03800000u;
+    const float m = __uint_as_float(mx), inv = none ? 0.f : 127.f / m;
+    if (lane == 0) as[row] = none ? 0.f : m / 127.f;
+    const float* src = a32 + (size_t)row * pitch;
     int8_t* dst = aq + (size_t)row * pitch;
     for (int c = lane; c < pitch / 8; c += 64) {
         uint2 o = make_uint2(0u, 0u);
         if (8 * c < f) {   // columns past f are zeros already, whole pieces of them were not written
-            const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * c);
-            const float k = gm[c / 4] * inv * (1.0f / 32767.f);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            const float4 lo = *reinterpret_cast<const float4*>(src + 8 * c), hi = *reinterpret_cast<const float4*>(src + 8 * c + 4);
+            const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             uint32_t p[2] = {0u, 0u};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float a = (float)(int16_t)(w[i / 2] >> (16 * (i & 1))) * k;
-                p[i / 4] |= ((uint32_t)(int)rintf(fminf(fmaxf(a, -127.f), 127.f)) & 0xffu) << (8 * (i & 3));
-            }
+            for (int i = 0; i < 8; ++i)
+                p[i / 4] |= ((uint32_t)(int)rintf(fminf(fmaxf(v[i] * inv, -127.f), 127.f)) & 0xffu) << (8 * (i & 3));
             o = make_uint2(p[0], p[1]);
         }
         *reinterpret_cast<uint2*>(dst + 8 * c) = o;
@@ -849,8 +830,8 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
     char* p = (char*)ws;
     int32_t* map = (int32_t*)p;
     p += ffn_q8_tilemap_bytes(B, E);
-    int16_t* a16 = (int16_t*)p;
-    p += align_up((size_t)B * fp * 2, 256);
+    float* a32 = (float*)p;
+    p += align_up((size_t)B * fp * 4, 256);
     float* gmax = (float*)p;
     p += align_up((size_t)B * (fp / kQ8Group) * 4, 256);
     int8_t* aq = (int8_t*)p;
@@ -863,7 +844,7 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
     int st = launch_tile_map(expert_offsets, E, tile_rows, max_tiles, map, map + ffn_q8_sched_offset(B, E), false, s);
     if (st != XMOE_OK) return st;
     const Q8Args up = {(const int8_t*)xq, x_scale, row_index, expert_offsets, map, (const int8_t*)wgq, (const int8_t*)wuq,
-                       g_scale, u_scale, dp, f, tile_rows, kQ8RowTiles, a16, gmax, fp, nullptr};
+                       g_scale, u_scale, dp, f, tile_rows, kQ8RowTiles, a32, gmax, fp, nullptr};
     const Q8Args down = {aq, as, nullptr, expert_offsets, map, (const int8_t*)wdq, nullptr, d_scale, nullptr, fp, d, tile_rows,
                          kQ8RowTiles, nullptr, nullptr, 0, y};
     st = tile_rows == 256   ? launch_q8_gateup<256, 8>(up, max_tiles, s)
@@ -871,7 +852,7 @@ int xmoe_expert_ffn_q8_fwd(const void* xq, const float* x_scale, const int32_t* 
                             : launch_q8_gateup_few(up, max_tiles, s);
     if (st != XMOE_OK) return st;
     XMOE_LAUNCH(K_Q8_ROWS, s,
-                hipLaunchKernelGGL(q8_rows_kernel, dim3((unsigned)((B + 3) / 4)), dim3(256), 0, s, a16, gmax, expert_offsets,
+                hipLaunchKernelGGL(q8_rows_kernel, dim3((unsigned)((B + 3) / 4)), dim3(256), 0, s, a32, gmax, expert_offsets,
                                    E, f, fp, aq, as));
     return tile_rows == 256   ? launch_q8_down<256, 8>(down, max_tiles, dt, s)
            : tile_rows == 128 ? launch_q8_down<128, 4>(down, max_tiles, dt, s)

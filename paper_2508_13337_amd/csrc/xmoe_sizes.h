@@ -85,7 +85,7 @@ static inline size_t gate_bwd_ws_bytes(int T, int d, int E) {
 // ----- 8-bit rows: bytes of a row of n values -----
 static inline int q8_pitch(int n) { return (n + 127) / 128 * 128; }
 
-// ----- experts on 8-bit integers: tile map | A as 16-bit integers, the maxima of every 32 columns | A's 8-bit rows, scales
+// ----- experts on 8-bit integers: tile map | A in float32, the maxima of every 32 columns | A's 8-bit rows, scales
 // The tile map for tiles of down to 32 rows, the schedule block that comes with it behind.
 constexpr int kQ8MinRowTile = 32;
 static inline size_t ffn_q8_sched_offset(int B, int E) { return 4 + 2 * (size_t)ffn_max_tiles(B, E, kQ8MinRowTile); }
@@ -94,7 +94,7 @@ static inline size_t ffn_q8_tilemap_bytes(int B, int E) {
 }
 static inline size_t ffn_q8_ws_bytes(int B, int E, int f) {
     const size_t b = B > 0 ? B : 1, fp = q8_pitch(f);
-    return ffn_q8_tilemap_bytes(B, E) + align_up(b * fp * 2, 256) + align_up(b * (fp / 32) * 4, 256) + align_up(b * fp, 256) +
+    return ffn_q8_tilemap_bytes(B, E) + align_up(b * fp * 4, 256) + align_up(b * (fp / 32) * 4, 256) + align_up(b * fp, 256) +
            align_up(b * 4, 256);
 }
 
