@@ -383,7 +383,7 @@ int xmoe_q8_pitch(int n);
 /* Weights as 8-bit integers with one scale for each output column, for xmoe_expert_ffn_q8_fwd: for each expert e and
  * column n, m = max_k |w[e,k,n]|,  wq[e,n,k] = rint(w[e,k,n] * (127 / m)),  scale[e,n] = m / 127   (0 where m < 2^-120).
  * w [E,K,N] dt ("in x out"); wq [E,N,xmoe_q8_pitch(K)] int8 (out), K-contiguous, zeros behind the first K of a row, 16-byte
- * aligned; scale [E,N] float32 (out).  Done once for a model's weights.  K <= XMOE_MAX_Q8_WIDTH, E <= 65535.
+ * aligned; scale [E,N] float32 (out).  Done once for a model's weights.  K <= XMOE_MAX_Q8_WIDTH, E <= 65535, N <= 2^30 - 64.
  */
 int xmoe_quantize_weights(const void* w, int E, int K, int N, int dt, void* wq, float* scale, void* stream);
 

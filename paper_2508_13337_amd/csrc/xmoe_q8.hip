@@ -800,7 +800,8 @@ extern "C" {
 int xmoe_quantize_weights(const void* w, int E, int K, int N, int dt, void* wq, float* scale, void* stream) {
     if (!dtype_ok(dt)) return XMOE_ERR_UNSUPPORTED;
     if (E < 1 || K < 1 || N < 1) return XMOE_ERR_INVALID_ARG;
-    if (E > 65535 || K > XMOE_MAX_Q8_WIDTH || N > (1 << 30)) return XMOE_ERR_UNSUPPORTED;
+    if (E > 65535 || K > XMOE_MAX_Q8_WIDTH) return XMOE_ERR_UNSUPPORTED;
+    if (((long)N + 63) / 64 * 256 >= (1l << 32)) return XMOE_ERR_UNSUPPORTED;   // a grid has fewer than 2^32 threads
     if (!w || !wq || !scale || (reinterpret_cast<uintptr_t>(wq) & 15u)) return XMOE_ERR_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
     const dim3 grid((unsigned)((N + 63) / 64), (unsigned)E);
