@@ -2,9 +2,10 @@
 //
 //   out[t] = sum_j p[t, e_j] FFN_{e_j}(x[t]) + sum_s FFN_{E+s}(x[t]) (+ addend[t]),   FFN_e(x) = (silu(x Wg) * (x Wu)) Wd
 //
-// Bound by the weights of the experts that some token picked: each is read once, for all of its tokens.  Nothing of the
-// routing goes through tables in memory: a token's choice is a few integers, and every block finds the active experts and
-// their tokens (a 32-bit mask per expert) in LDS by itself.
+// Bound by the weights of the experts that some token picked: on the matrix cores each is read once, for all of its tokens, on
+// the vector ALUs once for every 8 of them (float32) or 4 (bf16).  Nothing of the routing goes through tables in memory: a
+// token's choice is a few integers, and every block finds the active experts and their tokens (a 32-bit mask per expert) in LDS
+// by itself.
 //
 //   route   one block per token: logits in the fixed order of xmoe_gate_logits, top-k (large routers: that call and xmoe_route)
 //   up      A = silu(x Wg) * (x Wu) of an active expert and 64 or 128 of its columns
@@ -13,8 +14,10 @@
 //
 // Two families of products: bf16 with widths that are multiples of 8 on the matrix cores, weights on a ring of direct-to-LDS
 // stages; everything else on the vector ALUs, where 16 groups of threads share a tile's K and read the weights straight to
-// registers.  d 2048, f 1408, 6 of 64 experts + 2, bf16: one token 45 us (11.8 + 19.5 + 10.4 + 4.1 and the gaps; 139 MB in up and
-// down at 4.6 TB/s), 16 tokens 189 (11.4 + 113 + 58 + 4.9; 5.2 TB/s).
+// registers.  A is an operand of the matrix cores and so rounded to bf16, as in the layer for many tokens; sums are float32 up to
+// the result (its distance from 64-bit arithmetic: 0.0018, of which the result's own rounding is 0.0017).
+// d 2048, f 1408, 6 of 64 experts + 2, bf16: one token 48 us (12 + 20.6 + 10.8 + 4.9; 139 MB in up and down at 4.4 TB/s), 16
+// tokens 189 (12 + 113 + 58 + 5.4; 5.2 TB/s).
 // Tried: a launch less, the last block of a column's down tiles adding the rows (a fence by every block: slower), and one
 // launch for all of it with a ticket per item (an atomic on one address takes 60 to 75 ns: 71 us for one token).
 #include "xmoe_ffn.h"
@@ -627,12 +630,13 @@ int launch_layer_route(const LayerArgs& a, hipStream_t s) {
 }
 
 // A block per token reads the whole router through one CU: up to this many bytes of it.  The whole call, us, so | by
-// xmoe_gate_logits and xmoe_route: 256 KiB (d 2048, 64 experts) 1 token 27.8|28.9, 32 tokens 40.0|40.5; 512 KiB (d 2048, 128
-// experts) 33.8|29.2 and 55.9|51.3, (d 4096, 64) 41.8|41.4 and 72.4|73.4; 1 MiB 50.8|41.6.
+// xmoe_gate_logits and xmoe_route: 256 KiB (d 2048, 64 experts) 1 token 27.8|28.8, 8 tokens 31.1|30.9, 32 tokens 39.9|40.5;
+// 512 KiB (d 2048, 128 experts) 33.5|29.1 and 63.2|58.2 for 1 and 32, (d 4096, 64) 41.6|41.5 and 72.4|73.0; 1 MiB 50.5|41.6.
 constexpr size_t kRouteBytes = 256 << 10;
 // From this many tiles of 128 columns on, up takes them (rows of 256 bytes of either matrix) instead of 64.  The whole call, us,
-// 128 | 64 columns, d 2048, f 1408: 88 tiles 55.8|48.9, 154 65.4|71.4, 286 98.4|97.6, 550 137.8|143.6, 726 189|185; d 4096, f 14336:
-// 224 tiles 149|162, 896 329|342; d 4096, f 1024: 264 tiles 134|149; d 1024, f 512: 64 tiles 28.0|24.0, 256 50.4|54.7.
+// 128 | 64 columns, d 2048, f 1408: 88 tiles 55.5|48.7, 154 65.4|71.1, 286 97.9|96.8, 550 137|143, 726 189|184; d 4096, f 14336:
+// 224 tiles 148|160, 896 326|337; d 4096, f 1024: 264 tiles 134|148; d 1024, f 512: 64 tiles 28.1|24.0, 256 50.5|54.8.  (At 286
+// and 726 tiles 64 columns are 1 and 3 % better: no line in the number of tiles tells those from their neighbours.)
 constexpr long kWideTiles = 128;
 
 }  // namespace

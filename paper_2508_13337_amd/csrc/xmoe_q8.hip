@@ -164,7 +164,8 @@ struct Q8Args {
 };
 
 // Row tiles that go through the column tiles together.  The 32 CUs of an XCD then read 4 + 8 operand tiles at a time, not 1 + 32
-// (d 4096, f 14336, 8 experts with 512 rows each: 990 us, in fours 930; 33 experts, f 1024, 1241 mean rows: 655 and 637).
+// (d 4096, f 14336, 8 experts with 512 rows each: 1038 us, in fours 969; 33 experts, f 1024, 1241 mean rows: 663 either way; 66
+// experts, d 2048, f 1408, 993 mean rows: 814 and 821).
 constexpr int kQ8RowTiles = 4;
 // Tile L: row tiles x column tiles, in groups of `group` row tiles (those of a column tile, then the next column tile), dealt to
 // the XCDs in eight runs of equal length (workgroup L goes to XCD L % 8): tiles in flight together share their weights
@@ -194,10 +195,10 @@ long q8_blocks(int N, int cols, int max_tiles) { return ((long)max_tiles * ((N +
 // five slots, two to three of them on their way.
 //   256: 8 waves (2 x 4) of 128 x 64 each, 160 KiB, one block per CU: the most products per byte of LDS.  A block takes tile
 //        after tile, and the units of the next one follow those of this one without a pause (66 experts, d 2048, f 1408, 993
-//        mean rows: a block per tile 463 us for gate/up, 254 for down, this way 457 and 244: 1.65 POP/s, where a large library
-//        product has 2.08).  Matrix cores are busy 43 % of it: a pass reads 192 KiB of LDS and writes 64, as long at 128 bytes a
-//        clock as its matrix instructions take, and the two overlap in part only.  (Waves of higher priority in their matrix
-//        instructions: 1 to 2 % slower.)
+//        mean rows: a block per tile 496 us for gate/up, 256 for down, this way 478 and 245: 1.57 POP/s, where a large library
+//        product has 2.08).  Matrix cores are busy 41 % of it.  LDS does not hold it up, by its counter: active 15 % of the
+//        clocks; waves wait 3 % of their time for its issue, 32 % for loads and barriers and 45 % for the issue of an
+//        instruction of any kind.  (Waves of higher priority in their matrix instructions: 1 to 2 % slower.)
 //   128: 4 waves (2 x 2) of 64 x 64 each, 80 KiB, two blocks per CU: where the weights' bytes are the bound, or 256 rows few
 // =========================================================================================================
 template <int MT, int WAVES>
@@ -688,7 +689,7 @@ int launch_q8_down_few(const Q8Args& a, int max_tiles, int dt, hipStream_t s) {
 }
 
 // =========================================================================================================
-// A's 8-bit rows: one wave per row.  HBM-bound.
+// A's 8-bit rows: one wave per row.  HBM-bound: 65536 rows, f 1408, 85 us, 5.4 TB/s.
 // =========================================================================================================
 __global__ __launch_bounds__(256) void q8_rows_kernel(const float* __restrict__ a32, const float* __restrict__ gmax,
                                                       const int32_t* __restrict__ off, int E, int f, int pitch,
@@ -716,7 +717,8 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const float* __restrict__ 
     for (int c = lane; c < pitch / 8; c += 64) {
         uint2 o = make_uint2(0u, 0u);
         if (8 * c < f) {   // columns past f are zeros already, whole pieces of them were not written
-            const float4 lo = *reinterpret_cast<const float4*>(src + 8 * c), hi = *reinterpret_cast<const float4*>(src + 8 * c + 4);
+            const float4 lo = *reinterpret_cast<const float4*>(src + 8 * c);
+            const float4 hi = *reinterpret_cast<const float4*>(src + 8 * c + 4);
             const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             uint32_t p[2] = {0u, 0u};
 #pragma unroll
@@ -729,8 +731,10 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const float* __restrict__ 
 }
 
 // =========================================================================================================
-// Weights [K, N] ("in x out") of an expert -> [N, pitch] integers and one scale per column.  Done once for a model's weights:
-// a block owns 64 columns, reads them twice (maximum, then integers) and turns 64 x 64 pieces over in LDS.
+// Weights [K, N] ("in x out") of an expert -> [N, pitch] integers and one scale per column.  Done once for a model's weights,
+// so it is simple: a block owns 64 columns, reads them twice (maximum, then integers) and turns 64 x 64 pieces over in LDS.
+// 66 matrices of 2048 x 1408 in bf16: 407 us, 2.3 TB/s of what it reads and writes; read once, they would take 96 at memory's
+// rate.
 // =========================================================================================================
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restrict__ w, int K, int N, int pitch,
@@ -771,18 +775,21 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restri
 }
 
 
-// Rows of a tile, by the mean load.  Measured (MI355X, all launches together, us, 256 | 128 | 32):
-//     mean rows                         1 - 2       8          16          62       124      155      186      248      496
-//     64 experts + 2, d 2048, f 1408  122|99|88  177|149|131  174|153|142  190|180  229|205  240|232  260|288  270|302  426|533
-//     8 experts, d 2048, f 1408                                                                                74|60    83|95
-//     8 experts, d 4096, f 14336                                                    440|466                   582|703  939| -
-//     256 experts, d 2048, f 512                                          266|247                             423|518
-//     24 experts, d 1000, f 712, Zipf                                                                60|55     68|64
-//     32 experts + 1, d 4096, f 1024                                                         201|189          233|272 (310)
-//     16 experts + 1, d 7168, f 2048                                                                302|292
-// (32-row tiles at 31 and 47 mean rows of 64 experts + 2: 155 for 128 rows' 156, 190 for 171.)  Up to 384 rows the larger tile
-// also has to come out at one tile for every CU; and K has two units or more, as the next tile's first are requested with
-// this one's last.
+// Rows of a tile, by the mean load.  Measured (MI355X, the whole call, us, 256 | 128 | 32):
+//     mean rows                         1           8            16           31           47           62
+//     64 experts + 2, d 2048, f 1408  108|89|77  160|140|126  165|142|136  172|151|147  176|166|179  185|173|200
+//     256 experts, d 2048, f 512                                                                     254|241|295
+//     mean rows                         124      155      186      248      310      496
+//     64 experts + 2, d 2048, f 1408  219|201  230|229  248|289  261|304           427|556
+//     8 experts, d 2048, f 1408                          62|44    65|53
+//     8 experts, d 4096, f 14336      421|442                    524|645           863|1006
+//     256 experts, d 2048, f 512      290|315                    413|501
+//     24 experts, d 1000, f 712, Zipf  51|37              52|49    56|54
+//     32 experts + 1, d 4096, f 1024           196|184           216|214  231|273
+//     16 experts + 1, d 7168, f 2048           293|281           313|320
+// Up to 384 rows the larger tile also has to come out at one tile for every CU; and K has two units or more, as the next tile's
+// first are requested with this one's last.  The mean is all that the rule goes by: at 124 rows of wide experts or of many it
+// loses 5 and 8 % so, 3 % at 31 rows and 1 to 4 % at 248 of a skewed load or few tiles.
 int q8_tile_rows(int B, int E, int d, int f) {
     if (B <= 16ll * E) return 32;
     const long tiles = ((long)B / 256 + E) * ((f + 127) / 128);
